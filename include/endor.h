@@ -449,6 +449,129 @@ endor_status endor_pipeline_destroy(endor_pipeline *p);
  */
 endor_status endor_h2d_decompress_pipeline(endor_pipeline *p, const endor_host_blob *blobs, int count);
 
+/*
+ * ---------------------------------------------------------------------------------------------
+ * THE DECODE SIDE.  What one token of generation needs beside the products with the compressed
+ * weight: a paged cache of keys and values with the attention that reads it, the write of new
+ * tokens, eviction by accumulated attention weight; and products with 4-bit weights (Section 4.2
+ * joins pruning with quantization).
+ *
+ * A cache is a pool of pages; a page holds `page_size` slots of every kv head, and element d
+ * of the key in slot s of head h of page p lies at d_k[p*page_stride + h*head_stride + s*slot_stride + d]
+ * (values likewise in d_v; strides in elements).  Slot t of sequence b is slot t % page_size of
+ * page d_pages[b*pages_stride + t / page_size].  Lengths are device arrays, so that a captured
+ * graph can be replayed while they grow; the host only knows bounds.  A sequence's capacity is
+ * max_pages * page_size, and no more than that many of its slots are ever looked at.  An entry of
+ * d_pages outside [0, num_pages) is a page that is not there: its slots are neither read nor written.
+ *
+ * Beside the cache a program may keep, per sequence, kv head and slot, an accumulated attention weight
+ * (fp32) and the position in the sequence of the token that lies there (int32): arrays [batch][kv_heads][capacity].
+ */
+enum { ENDOR_F16 = 0, ENDOR_BF16 = 1 };
+
+typedef struct endor_kv_cache {
+    void *d_k, *d_v;        /* 16-byte aligned */
+    int64_t page_stride, head_stride, slot_stride; /* elements; multiples of 8, at least head_dim */
+    int64_t num_pages;      /* pages in the pool, < 2^31 */
+    const int32_t *d_pages; /* [batch][max_pages] */
+    int64_t pages_stride;   /* elements between its rows */
+    int32_t batch, kv_heads;
+    int32_t head_dim;       /* a multiple of 8, 8 to 256 */
+    int32_t page_size;      /* a power of two, 8 to 32768 */
+    int32_t max_pages;      /* max_pages * page_size < 2^31 */
+    int32_t dtype;          /* ENDOR_F16 or ENDOR_BF16: keys, values, queries and attention outputs */
+} endor_kv_cache;
+
+/*
+ * DEVICE.  Append: token t < min(counts[b], tokens) of sequence b goes to slot lengths[b] + t.
+ *   d_k_new, d_v_new  element d of token t, head h of sequence b at b*seq_stride + t*token_stride + h*head_stride + d
+ *                     (the cache's type, element-aligned; strides in elements)
+ *   d_counts          [batch] or NULL: every sequence brings `tokens`
+ *   d_lengths, d_seen [batch]: slots in use, and tokens seen so far (more than lengths after eviction)
+ *   d_lengths_out, d_seen_out   [batch]: both advanced by the tokens stored; may be the arrays above
+ *   d_weights, d_positions      [batch][kv_heads][capacity] or NULL: the new slots' weight is set to 0,
+ *                     their position to seen[b] + t
+ * Tokens past the capacity are not stored.  Pages that a sequence appends to must be its own.
+ */
+endor_status endor_kv_append(const endor_kv_cache *cache, const void *d_k_new, const void *d_v_new,
+                             int64_t seq_stride, int64_t token_stride, int64_t head_stride, int tokens,
+                             const int32_t *d_counts, const int32_t *d_lengths, const int32_t *d_seen,
+                             int32_t *d_lengths_out, int32_t *d_seen_out,
+                             float *d_weights, int32_t *d_positions, void *stream);
+
+/*
+ * DEVICE.  Attention of one new token per sequence over the cache: for query head h of sequence b, which
+ * reads kv head h / (q_heads / kv_heads),
+ *     s_t = scale * <q, k_t>,  p_t = exp(s_t - lse),  lse = log sum_t exp(s_t),  out = sum_t p_t v_t
+ * over the slots t < min(lengths[b], max_len) that are visible.  Sums and softmax statistics are held in fp32.
+ *   d_q          element d of head h of sequence b at b*q_seq_stride + h*q_head_stride + d
+ *   max_len      host's bound on the lengths (longer sequences are read up to it); the work is laid out by it
+ *   d_mask       NULL, or a bitmap of the slots of every sequence, bit (t & 63) of word
+ *                d_mask[b*mask_stride + (t >> 6)]: 0 = slot t is not visible.  What lies in slots that are not
+ *                visible, past the length or on pages that are not there does not matter, NaN included.
+ *   d_out        [batch][q_heads][head_dim], of the cache's type; zeros where no slot is visible
+ *   d_lse        [batch][q_heads] fp32 or NULL; -infinity where no slot is visible
+ *   d_weights, d_weights_out   NULL, or [batch][kv_heads][capacity]: weights_out[t] = weights[t] + the sum of p_t
+ *                over the query heads that share the kv head, for all t < min(lengths[b], max_len); slots past that
+ *                are left alone.  d_weights may be d_weights_out, or NULL (then taken as 0).
+ *   d_scratch    endor_attn_scratch_bytes() bytes, 256-byte aligned (NULL when that is 0)
+ * q_heads is a multiple of kv_heads.  A visible slot whose key or value is not finite makes outputs that are not finite.
+ */
+size_t endor_attn_scratch_bytes(const endor_kv_cache *cache, int q_heads, int32_t max_len, int with_weights);
+endor_status endor_attn_decode(const endor_kv_cache *cache, int q_heads,
+                               const void *d_q, int64_t q_seq_stride, int64_t q_head_stride,
+                               const int32_t *d_lengths, int32_t max_len,
+                               const uint64_t *d_mask, int64_t mask_stride, float scale,
+                               void *d_out, float *d_lse, const float *d_weights, float *d_weights_out,
+                               void *d_scratch, size_t scratch_bytes, void *stream);
+
+/*
+ * DEVICE.  Eviction: every sequence of more than `budget` slots is brought down to `budget`, each kv head by its own
+ * weights.  Tokens of positions >= seen[b] - recent stay; of the others those of the largest weights do (of equal ones
+ * the lowest slot's; NaN is least; should tokens of such positions be more than the budget, the lowest slots of them
+ * stay).  A kept token in a slot below the budget stays where it is; the i-th kept token
+ * past it moves into the i-th slot that has come free below it, with its key, value, weight and position.  So the
+ * order of slots is not the order of tokens afterwards (attention does not depend on it; a mask by slots does).
+ *   d_lengths, d_lengths_out      [batch]; may be the same array
+ *   d_weights, d_positions        [batch][kv_heads][capacity]
+ *   d_weights_out, d_positions_out  likewise, slots below the new length written; may be the arrays above
+ *   max_len      host's bound on the lengths (longer sequences are taken to have max_len slots)
+ *   d_scratch    endor_kv_evict_scratch_bytes() bytes, 256-byte aligned (NULL when that is 0)
+ * 0 <= recent <= budget.  Pages that a sequence holds must be its own.
+ */
+size_t endor_kv_evict_scratch_bytes(const endor_kv_cache *cache, int32_t budget, int32_t max_len);
+endor_status endor_kv_evict(const endor_kv_cache *cache, int32_t budget, int32_t recent, int32_t max_len,
+                            const int32_t *d_lengths, const int32_t *d_seen,
+                            const float *d_weights, const int32_t *d_positions,
+                            int32_t *d_lengths_out, float *d_weights_out, int32_t *d_positions_out,
+                            void *d_scratch, size_t scratch_bytes, void *stream);
+
+/*
+ * 4-BIT WEIGHTS.  W[i][j] = (code[i][j] - zero[i][j / group]) * scale[i][j / group], codes and zeros whole numbers
+ * from 0 to 15, scales fp16; without zeros, 8 everywhere.  `group` is a power of two, 32 to 32768; the last group of a
+ * row may be partial.  A checkpoint's form is d_codes: rows of (cols + 1) / 2 bytes, the even column in the low half;
+ * d_scales, d_zeros (one byte each): [rows][ceil(cols / group)].  The products read a packed form, laid out once by
+ * endor_q4_pack into endor_q4_bytes() bytes (256-byte aligned; 0 on bad arguments).  rows*cols < 2^34, rows and cols < 2^26.
+ *
+ * endor_q4_quantize makes a checkpoint's form of a dense fp16 matrix (rows*cols elements, contiguous) by rounding to
+ * nearest: with d_zeros from the smallest and largest value of a group (0 among them), without symmetrically.
+ */
+size_t endor_q4_bytes(int64_t rows, int64_t cols, int group, int with_zeros);
+endor_status endor_q4_pack(int64_t rows, int64_t cols, int group, const uint8_t *d_codes, const uint16_t *d_scales,
+                           const uint8_t *d_zeros, void *d_packed, size_t packed_bytes, void *stream);
+endor_status endor_q4_quantize(int64_t rows, int64_t cols, int group, const uint16_t *d_dense, uint8_t *d_codes,
+                               uint16_t *d_scales, uint8_t *d_zeros, void *stream);
+
+/*
+ * DEVICE.  Y = X W^T for nb <= ENDOR_GEMM_MAX_BATCH right-hand sides with a packed 4-bit W.
+ *   d_x      nb vectors of cols elements of `dtype` (ENDOR_F16 or ENDOR_BF16), vector b at d_x + b*ldx (ldx >= cols)
+ *   d_y      out, nb x rows fp32: the sums of (code - zero)*x over a group are exact products summed in fp32, then
+ *            multiplied by the group's scale and summed in fp32, in a fixed order: results are the same from run to run
+ * 16-byte aligned d_x with ldx a multiple of 8 selects the fast load path.
+ */
+endor_status endor_q4_gemm(int64_t rows, int64_t cols, int group, int with_zeros, const void *d_packed, size_t packed_bytes,
+                           int dtype, const void *d_x, int64_t ldx, int nb, float *d_y, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,6 +15,9 @@ SOURCES = [os.path.join(HERE, "csrc", "endor_kernels.hip"),
            os.path.join(HERE, "csrc", "endor_gemm.hip"),
            os.path.join(HERE, "csrc", "endor_gemv.hip"),
            os.path.join(HERE, "csrc", "endor_pipeline.hip"),
+           os.path.join(HERE, "csrc", "endor_attn.hip"),
+           os.path.join(HERE, "csrc", "endor_kv.hip"),
+           os.path.join(HERE, "csrc", "endor_q4.hip"),
            os.path.join(HERE, "csrc", "endor_host.cpp")]
 # the streaming yardstick kernels bench.py times beside the library (not part of the product path)
 PROBE_LIB = os.path.join(HERE, "libendor_probe.so")
