@@ -478,7 +478,7 @@ typedef struct endor_kv_cache {
     int32_t batch, kv_heads;
     int32_t head_dim;       /* a multiple of 8, 8 to 256 */
     int32_t page_size;      /* a power of two, 8 to 32768 */
-    int32_t max_pages;      /* max_pages * page_size < 2^31 */
+    int32_t max_pages;      /* max_pages * page_size <= 2^30 */
     int32_t dtype;          /* ENDOR_F16 or ENDOR_BF16: keys, values, queries and attention outputs */
 } endor_kv_cache;
 

@@ -28,7 +28,7 @@ inline endor_status read_cache(const endor_kv_cache *c, Cache *out) {
     if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8 != 0) return ENDOR_ERR_UNSUPPORTED;
     if (c->page_size < 8 || c->page_size > 32768 || (c->page_size & (c->page_size - 1)) != 0) return ENDOR_ERR_UNSUPPORTED;
     if (c->dtype != ENDOR_F16 && c->dtype != ENDOR_BF16) return ENDOR_ERR_UNSUPPORTED;
-    if (int64_t(c->max_pages) * c->page_size > 0x7fffffff) return ENDOR_ERR_UNSUPPORTED;
+    if (int64_t(c->max_pages) * c->page_size > (1 << 30)) return ENDOR_ERR_UNSUPPORTED;
     // a launch has at most 65535 workgroups in y and z, and a program of a few heads never comes near it
     if (c->batch > 65535 || c->kv_heads > 65535) return ENDOR_ERR_UNSUPPORTED;
     for (int64_t s : {c->page_stride, c->head_stride, c->slot_stride})
