@@ -10,11 +10,19 @@
 #include <cstdint>
 
 #include "endor.h"
+#include "endor_device.h"
 #include "endor_kv.h"
 
 namespace {
 
+using endor_device::u32x4;
 using endor_kv::aligned;
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 struct Layout {
     int64_t tiles, blocks, groups;  // groups: of a padded row
@@ -112,35 +120,170 @@ struct Q4Params {
     const uint8_t *zeros;
     const uint16_t *x;
     float *y;
-    int64_t rows, cols, ldx, blocks, groups;
-    uint32_t group_shift;
+    int64_t rows, cols, ldx;
+    uint32_t tiles, blocks, groups, per_group_shift, nb;  // per_group_shift: blocks of a group, where those are whole
+};
+
+// Eight codes as pairs of the type's numbers code - zero, which are exact: columns (0, 1), (2, 3), (4, 5), (6, 7).
+template <bool kBf16>
+struct Zero;  // what is taken off: prepared once per row and group
+template <>
+struct Zero<false> {
+    f16x2 near, far;
+    __device__ __forceinline__ explicit Zero(float z) {
+        near = f16x2{static_cast<_Float16>(-1024.0f - z), static_cast<_Float16>(-1024.0f - z)};
+        far = f16x2{static_cast<_Float16>(-64.0f - z), static_cast<_Float16>(-64.0f - z)};
+    }
+    // A code in the low bits of 0x6400 is the number 1024 + code, in the next four 1024 + 16 code.
+    __device__ __forceinline__ u32x4 operand(uint32_t w) const {
+        auto low = [](uint32_t v) { return __builtin_bit_cast(f16x2, (v & 0x000f000fu) | 0x64006400u); };
+        auto high = [](uint32_t v) { return __builtin_bit_cast(f16x2, (v & 0x00f000f0u) | 0x64006400u); };
+        const f16x2 sixteenth = {static_cast<_Float16>(0.0625f), static_cast<_Float16>(0.0625f)};
+        const uint32_t v = w >> 8;
+        return u32x4{__builtin_bit_cast(uint32_t, low(w) + near), __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(high(w), sixteenth, far)),
+                     __builtin_bit_cast(uint32_t, low(v) + near), __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(high(v), sixteenth, far))};
+    }
+};
+template <>
+struct Zero<true> {
+    float z;
+    __device__ __forceinline__ explicit Zero(float zero) : z(zero) {}
+    __device__ __forceinline__ u32x4 operand(uint32_t w) const {
+        const uint32_t low = w & 0x0f0f0f0fu, high = (w >> 4) & 0x0f0f0f0fu;  // columns 0, 4, 1, 5 and 2, 6, 3, 7
+        auto pair = [&](uint32_t v, int a) {  // a whole number below 16 has its bits in the upper half of a float
+            const float x = static_cast<float>((v >> (8 * a)) & 0xffu) - z, y = static_cast<float>((v >> (8 * a + 16)) & 0xffu) - z;
+            return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+        };
+        return u32x4{pair(low, 0), pair(high, 0), pair(low, 1), pair(high, 1)};
+    }
 };
 
 template <bool kBf16>
-__device__ __forceinline__ float widen(uint16_t x) {
-    if constexpr (kBf16) return __uint_as_float(uint32_t(x) << 16);
-    return static_cast<float>(__builtin_bit_cast(_Float16, x));
+__device__ __forceinline__ f32x4 product(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (kBf16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// One wave per row and right-hand side.
-template <bool kBf16>
-__global__ __launch_bounds__(64) void endor_q4_gemm_kernel(Q4Params Q) {
-    const int64_t row = blockIdx.x, tile = row / 16;
-    const uint16_t *x = Q.x + blockIdx.y * Q.ldx;
-    const uint32_t r = row & 15, lane = threadIdx.x;
-    float total = 0;
-    for (int64_t g = 0; g < Q.groups; ++g) {
-        float sum = 0;
-        const int64_t from = g << Q.group_shift, to = from + (int64_t(1) << Q.group_shift) < Q.cols ? from + (int64_t(1) << Q.group_shift) : Q.cols;
-        const float zero = Q.zeros ? Q.zeros[(tile * Q.groups + g) * 16 + r] : 8.0f;
-        for (int64_t c = from + lane; c < to; c += 64) {
-            const uint32_t in = c & 127, word = Q.codes[((tile * Q.blocks + c / 128) * 64 + (in / 8 % 4) * 16 + r) * 4 + in / 32];
-            sum += (float(word >> (4 * place_of(in & 7)) & 15u) - zero) * widen<kBf16>(x[c]);
+// A workgroup has kTiles row tiles; its waves take the blocks of 128 columns in turn and are joined in LDS.  kParts: groups of a block.
+// kAligned: rows of x begin at 16-byte boundaries.
+template <int kTiles, int kParts, bool kZeros, bool kBf16, bool kAligned>
+__global__ __launch_bounds__(512) void endor_q4_gemm_kernel(Q4Params Q) {
+    extern __shared__ float s_part[];  // [wave][right-hand side][16 kTiles rows]
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, n = lane & 15, g = lane >> 4;
+    const uint32_t tile0 = blockIdx.x * kTiles;
+    const uint16_t *x = Q.x + int64_t(n < Q.nb ? n : Q.nb - 1) * Q.ldx + 8 * g;  // columns past the last right-hand side are not stored
+
+    struct Block {
+        u32x4 codes[kTiles], x[4];
+        f16x4 scales[kTiles][kParts];
+        uint8_t zeros[kTiles][kZeros ? kParts : 1];
+    };
+    const uint32_t last = Q.blocks - 1;
+    auto load = [&](uint32_t block, Block &B) {
+        const uint32_t group = kParts > 1 ? block * kParts : block >> Q.per_group_shift;
+#pragma unroll
+        for (int r = 0; r < kTiles; ++r) {
+            const uint32_t tile = tile0 + r < Q.tiles ? tile0 + r : Q.tiles - 1;
+            B.codes[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(Q.codes) + (uint64_t(tile) * Q.blocks + block) * 64 + lane);
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                const uint64_t at = (uint64_t(tile) * Q.groups + group + p) * 16;
+                B.scales[r][p] = *reinterpret_cast<const f16x4 *>(Q.scales + at + 4 * g);
+                if constexpr (kZeros) B.zeros[r][p] = Q.zeros[at + n];
+            }
         }
-        total += sum * float(Q.scales[(tile * Q.groups + g) * 16 + r]);
+        const uint16_t *from = x + int64_t(block) * 128;
+        if (block < last || Q.cols % 128 == 0) {
+            typedef u32x4 u32x4_any __attribute__((aligned(2)));
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                B.x[j] = kAligned ? *reinterpret_cast<const u32x4 *>(from + 32 * j) : *reinterpret_cast<const u32x4_any *>(from + 32 * j);
+        } else {  // zeros past the last column
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const int64_t c = int64_t(block) * 128 + 32 * j + 8 * g + e;
+                    const uint32_t a = c < Q.cols ? from[32 * j + e] : 0, z = c + 1 < Q.cols ? from[32 * j + e + 1] : 0;
+                    B.x[j][e / 2] = a | z << 16;
+                }
+        }
+    };
+    f32x4 total[kTiles];
+#pragma unroll
+    for (int r = 0; r < kTiles; ++r) total[r] = f32x4{0, 0, 0, 0};
+    auto add = [&](const Block &B) {
+#pragma unroll
+        for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                const Zero<kBf16> zero(kZeros ? static_cast<float>(B.zeros[r][p]) : 8.0f);
+                f32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+                for (int j = 4 / kParts * p; j < 4 / kParts * (p + 1); ++j) sum = product<kBf16>(zero.operand(B.codes[r][j]), B.x[j], sum);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) total[r][i] += sum[i] * static_cast<float>(B.scales[r][p][i]);
+            }
+    };
+    if (wave < Q.blocks) {
+        Block a, z;
+        uint32_t block = wave;
+        load(block, a);
+        for (;;) {
+            const uint32_t second = block + waves, third = second + waves;
+            load(second < last ? second : last, z);
+            add(a);
+            if (second >= Q.blocks) break;
+            load(third < last ? third : last, a);
+            add(z);
+            if (third >= Q.blocks) break;
+            block = third;
+        }
     }
-    for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
-    if (lane == 0) Q.y[blockIdx.y * Q.rows + row] = total;
+    if (n < Q.nb)
+#pragma unroll
+        for (int r = 0; r < kTiles; ++r) *reinterpret_cast<f32x4 *>(s_part + ((wave * Q.nb + n) * kTiles + r) * 16 + 4 * g) = total[r];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < Q.nb * kTiles * 16; i += blockDim.x) {
+        float sum = 0;
+        for (uint32_t w = 0; w < waves; ++w) sum += s_part[w * Q.nb * kTiles * 16 + i];
+        const uint32_t b = i / (kTiles * 16);
+        const int64_t row = int64_t(tile0) * 16 + i % (kTiles * 16);
+        if (row < Q.rows) Q.y[b * Q.rows + row] = sum;
+    }
+}
+
+template <int kTiles, int kParts, bool kZeros, bool kBf16>
+void launch_aligned(const Q4Params &Q, uint32_t waves, hipStream_t s) {
+    const bool even = (reinterpret_cast<uintptr_t>(Q.x) & 15) == 0 && (Q.ldx % 8 == 0 || Q.nb == 1);
+    hipLaunchKernelGGL((even ? endor_q4_gemm_kernel<kTiles, kParts, kZeros, kBf16, true> : endor_q4_gemm_kernel<kTiles, kParts, kZeros, kBf16, false>),
+                       dim3((Q.tiles + kTiles - 1) / kTiles), dim3(64 * waves), waves * Q.nb * kTiles * 16 * sizeof(float), s, Q);
+}
+template <int kTiles, int kParts>
+void launch_kind(const Q4Params &Q, bool bf16, uint32_t waves, hipStream_t s) {
+    if (Q.zeros)
+        bf16 ? launch_aligned<kTiles, kParts, true, true>(Q, waves, s) : launch_aligned<kTiles, kParts, true, false>(Q, waves, s);
+    else
+        bf16 ? launch_aligned<kTiles, kParts, false, true>(Q, waves, s) : launch_aligned<kTiles, kParts, false, false>(Q, waves, s);
+}
+template <int kTiles>
+void launch_parts(const Q4Params &Q, int group, bool bf16, uint32_t waves, hipStream_t s) {
+    if (group == 32)
+        launch_kind<kTiles, 4>(Q, bf16, waves, s);
+    else if (group == 64)
+        launch_kind<kTiles, 2>(Q, bf16, waves, s);
+    else
+        launch_kind<kTiles, 1>(Q, bf16, waves, s);
+}
+void launch(const Q4Params &Q, int group, bool bf16, int tiles, uint32_t waves, hipStream_t s) {
+    if (tiles == 4)
+        launch_parts<4>(Q, group, bf16, waves, s);
+    else if (tiles == 2)
+        launch_parts<2>(Q, group, bf16, waves, s);
+    else
+        launch_parts<1>(Q, group, bf16, waves, s);
 }
 
 }  // namespace
@@ -222,10 +365,11 @@ extern "C" endor_status endor_q4_gemm(int64_t rows, int64_t cols, int group, int
     Q.rows = rows;
     Q.cols = cols;
     Q.ldx = ldx;
-    Q.blocks = l.blocks;
-    Q.groups = l.groups;
-    Q.group_shift = static_cast<uint32_t>(__builtin_ctz(static_cast<unsigned>(group)));
-    hipLaunchKernelGGL(dtype == ENDOR_BF16 ? endor_q4_gemm_kernel<true> : endor_q4_gemm_kernel<false>, dim3(static_cast<uint32_t>(rows), nb), dim3(64),
-                       0, s, Q);
+    Q.tiles = static_cast<uint32_t>(l.tiles);
+    Q.blocks = static_cast<uint32_t>(l.blocks);
+    Q.groups = static_cast<uint32_t>(l.groups);
+    Q.per_group_shift = group > 128 ? static_cast<uint32_t>(__builtin_ctz(static_cast<unsigned>(group))) - 7 : 0;
+    Q.nb = static_cast<uint32_t>(nb);
+    launch(Q, group, dtype == ENDOR_BF16, l.tiles >= 1024 ? 2 : 1, 8, s);
     return hipGetLastError() == hipSuccess ? ENDOR_OK : ENDOR_ERR_HIP;
 }
