@@ -567,10 +567,13 @@ endor_status endor_q4_quantize(int64_t rows, int64_t cols, int group, const uint
  *   d_x      nb vectors of cols elements of `dtype` (ENDOR_F16 or ENDOR_BF16), vector b at d_x + b*ldx (ldx >= cols)
  *   d_y      out, nb x rows fp32: the sums of (code - zero)*x over a group are exact products summed in fp32, then
  *            multiplied by the group's scale and summed in fp32, in a fixed order: results are the same from run to run
+ *   d_scratch  endor_q4_scratch_bytes() bytes, 256-byte aligned (NULL when that is 0): sums of parts of the columns
  * 16-byte aligned d_x with ldx a multiple of 8 selects the fast load path.
  */
+size_t endor_q4_scratch_bytes(int64_t rows, int64_t cols, int group, int nb);
 endor_status endor_q4_gemm(int64_t rows, int64_t cols, int group, int with_zeros, const void *d_packed, size_t packed_bytes,
-                           int dtype, const void *d_x, int64_t ldx, int nb, float *d_y, void *stream);
+                           int dtype, const void *d_x, int64_t ldx, int nb, float *d_y,
+                           void *d_scratch, size_t scratch_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -2,21 +2,26 @@
 //
 // PACKED FORM.  Rows go in tiles of 16, columns in blocks of 128, both padded with codes and scales of zero, so that no
 // kernel has an edge in W.  Codes: [tile][block][lane 0..63][16 bytes]; lane l has row l & 15 of the tile, and its 32-bit word j the
-// columns 32 j + 8 (l >> 4) + 0..7 of the block, column c in bits 4 * kNibble[c].  Then the scales, fp16 [tile][group][16 rows],
-// then, if there are any, the zeros, a byte [tile][group][16 rows].  A block and a group that holds several blocks end
+// columns 32 j + 8 (l >> 4) + 0..7 of the block, column c in bits 4 * kNibble[c].  Then the scales, fp16, for a tile and a block (or a
+// group that holds blocks): [4 quarters][groups of the block][4 rows], as the lanes of a product's result want them; then, if there
+// are any, the zeros, bytes [16 rows][groups of the block], as the lanes of its operand do.  A block and a group that holds several blocks end
 // at the same column.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "endor.h"
 #include "endor_device.h"
 #include "endor_kv.h"
+#include "endor_q4_plan.h"
 
 namespace {
 
 using endor_device::u32x4;
 using endor_kv::aligned;
+using endor_q4_plan::make_plan;
+using endor_q4_plan::Plan;
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
@@ -75,10 +80,13 @@ __global__ __launch_bounds__(256) void endor_q4_pack_kernel(PackParams P) {
     }
     const int64_t entries = P.tiles * P.padded_groups * 16;
     if (i < entries) {
-        const int64_t row = i / (16 * P.padded_groups) * 16 + (i & 15), g = (i >> 4) % P.padded_groups;
-        const bool in = row < P.rows && g < P.groups;
-        P.out_scales[i] = in ? P.scales[row * P.groups + g] : 0;
-        if (P.out_zeros) P.out_zeros[i] = in ? P.zeros[row * P.groups + g] & 15 : 0;
+        const int64_t of_tile = 16 * P.padded_groups, tile = i / of_tile, parts = P.group < 128 ? 128 / P.group : 1;
+        const int64_t base = i % of_tile / (16 * parts) * parts;  // the first group of the block, or the group
+        const int64_t in = i % (16 * parts);
+        auto source = [&](int64_t r, int64_t g) { return 16 * tile + r < P.rows && g < P.groups ? (16 * tile + r) * P.groups + g : -1; };
+        const int64_t s = source(in / (4 * parts) * 4 + in % 4, base + in / 4 % parts), z = source(in / parts, base + in % parts);
+        P.out_scales[i] = s >= 0 ? P.scales[s] : 0;
+        if (P.out_zeros) P.out_zeros[i] = z >= 0 ? P.zeros[z] & 15 : 0;
     }
 }
 
@@ -121,42 +129,81 @@ struct Q4Params {
     const uint16_t *x;
     float *y;
     int64_t rows, cols, ldx;
+    float *partial;  // [split][nb][rows], where there are several
     uint32_t tiles, blocks, groups, per_group_shift, nb;  // per_group_shift: blocks of a group, where those are whole
+    uint32_t splits, per_split;  // parts of the columns, and blocks of one
 };
 
 // Eight codes as pairs of the type's numbers code - zero, which are exact: columns (0, 1), (2, 3), (4, 5), (6, 7).
-template <bool kBf16>
-struct Zero;  // what is taken off: prepared once per row and group
-template <>
-struct Zero<false> {
+struct Pairs {  // fp16
     f16x2 near, far;
-    __device__ __forceinline__ explicit Zero(float z) {
+    uint32_t mask, one;  // kept in registers, so that a pair takes one instruction
+    __device__ __forceinline__ explicit Pairs(float z) : mask(0x000f000fu), one(0x64006400u) {
         near = f16x2{static_cast<_Float16>(-1024.0f - z), static_cast<_Float16>(-1024.0f - z)};
         far = f16x2{static_cast<_Float16>(-64.0f - z), static_cast<_Float16>(-64.0f - z)};
+        asm("" : "+s"(mask));
+        asm("" : "+v"(one));
     }
     // A code in the low bits of 0x6400 is the number 1024 + code, in the next four 1024 + 16 code.
-    __device__ __forceinline__ u32x4 operand(uint32_t w) const {
-        auto low = [](uint32_t v) { return __builtin_bit_cast(f16x2, (v & 0x000f000fu) | 0x64006400u); };
-        auto high = [](uint32_t v) { return __builtin_bit_cast(f16x2, (v & 0x00f000f0u) | 0x64006400u); };
+    __device__ __forceinline__ void get(uint32_t w, f16x2 p[4]) const {
         const f16x2 sixteenth = {static_cast<_Float16>(0.0625f), static_cast<_Float16>(0.0625f)};
+        uint32_t high = mask << 4;
         const uint32_t v = w >> 8;
-        return u32x4{__builtin_bit_cast(uint32_t, low(w) + near), __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(high(w), sixteenth, far)),
-                     __builtin_bit_cast(uint32_t, low(v) + near), __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(high(v), sixteenth, far))};
+        p[0] = __builtin_bit_cast(f16x2, (w & mask) | one) + near;
+        p[1] = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (w & high) | one), sixteenth, far);
+        p[2] = __builtin_bit_cast(f16x2, (v & mask) | one) + near;
+        p[3] = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (v & high) | one), sixteenth, far);
+    }
+};
+template <bool kBf16, bool kZeros>
+struct Operand;  // of a row and group; what it makes of a code, times kUnit, is the number wanted
+template <bool kZeros>
+struct Operand<false, kZeros> {
+    static constexpr float kUnit = 1.0f;
+    Pairs pairs;
+    __device__ __forceinline__ explicit Operand(float z) : pairs(z) {}
+    __device__ __forceinline__ u32x4 of(uint32_t w) const {
+        f16x2 p[4];
+        pairs.get(w, p);
+        return u32x4{__builtin_bit_cast(uint32_t, p[0]), __builtin_bit_cast(uint32_t, p[1]), __builtin_bit_cast(uint32_t, p[2]), __builtin_bit_cast(uint32_t, p[3])};
     }
 };
 template <>
-struct Zero<true> {
-    float z;
-    __device__ __forceinline__ explicit Zero(float zero) : z(zero) {}
-    __device__ __forceinline__ u32x4 operand(uint32_t w) const {
-        const uint32_t low = w & 0x0f0f0f0fu, high = (w >> 4) & 0x0f0f0f0fu;  // columns 0, 4, 1, 5 and 2, 6, 3, 7
-        auto pair = [&](uint32_t v, int a) {  // a whole number below 16 has its bits in the upper half of a float
-            const float x = static_cast<float>((v >> (8 * a)) & 0xffu) - z, y = static_cast<float>((v >> (8 * a + 16)) & 0xffu) - z;
+struct Operand<true, true> {
+    static constexpr float kUnit = 1.0f;
+    Pairs pairs;
+    __device__ __forceinline__ explicit Operand(float z) : pairs(z) {}
+    __device__ __forceinline__ u32x4 of(uint32_t w) const {
+        f16x2 p[4];
+        pairs.get(w, p);
+        u32x4 out;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // whole numbers below 16 have their bits in the upper half of a float
+            const float x = static_cast<float>(p[i][0]), y = static_cast<float>(p[i][1]);
+            out[i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+        }
+        return out;
+    }
+};
+template <>
+struct Operand<true, false> {  // code - 8, of which the instruction makes a sixteenth
+    static constexpr float kUnit = 16.0f;
+    __device__ __forceinline__ explicit Operand(float) {}
+    __device__ __forceinline__ u32x4 of(uint32_t w) const {
+        const uint32_t low = w ^ 0x88888888u, high = low >> 4;
+        auto pair = [&](uint32_t v, int a) {
+            const float x = __builtin_amdgcn_cvt_off_f32_i4(v >> (8 * a)), y = __builtin_amdgcn_cvt_off_f32_i4(v >> (8 * a + 16));
             return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
         };
         return u32x4{pair(low, 0), pair(high, 0), pair(low, 1), pair(high, 1)};
     }
 };
+
+// Scales of four rows, zeros of one, of a block's groups.
+template <int kParts>
+using Scales = _Float16 __attribute__((ext_vector_type(4 * kParts)));
+template <int kParts>
+using Bytes = std::conditional_t<kParts == 4, uint32_t, std::conditional_t<kParts == 2, uint16_t, uint8_t>>;
 
 template <bool kBf16>
 __device__ __forceinline__ f32x4 product(u32x4 a, u32x4 b, f32x4 c) {
@@ -166,82 +213,49 @@ __device__ __forceinline__ f32x4 product(u32x4 a, u32x4 b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// A workgroup has kTiles row tiles; its waves take the blocks of 128 columns in turn and are joined in LDS.  kParts: groups of a block.
-// kAligned: rows of x begin at 16-byte boundaries.
-template <int kTiles, int kParts, bool kZeros, bool kBf16, bool kAligned>
-__global__ __launch_bounds__(512) void endor_q4_gemm_kernel(Q4Params Q) {
-    extern __shared__ float s_part[];  // [wave][right-hand side][16 kTiles rows]
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, n = lane & 15, g = lane >> 4;
-    const uint32_t tile0 = blockIdx.x * kTiles;
-    const uint16_t *x = Q.x + int64_t(n < Q.nb ? n : Q.nb - 1) * Q.ldx + 8 * g;  // columns past the last right-hand side are not stored
+// What a wave has of W on its way: a block of 128 columns of kTiles row tiles, with the scales and zeros of its groups (kParts of them).
+template <int kTiles, int kParts, bool kZeros>
+struct Block {
+    u32x4 codes[kTiles];
+    Scales<kParts> scales[kTiles];
+    Bytes<kParts> zeros[kZeros ? kTiles : 1];
 
-    struct Block {
-        u32x4 codes[kTiles], x[4];
-        f16x4 scales[kTiles][kParts];
-        uint8_t zeros[kTiles][kZeros ? kParts : 1];
-    };
-    const uint32_t last = Q.blocks - 1;
-    auto load = [&](uint32_t block, Block &B) {
+    // Tiles past the last one and blocks past `last` stand for it; what is loaded of them is not used.
+    __device__ __forceinline__ void load(const Q4Params &Q, uint32_t tile0, uint32_t wanted, uint32_t last, uint32_t lane) {
+        const uint32_t n = lane & 15, g = lane >> 4, block = wanted < last ? wanted : last;
         const uint32_t group = kParts > 1 ? block * kParts : block >> Q.per_group_shift;
 #pragma unroll
         for (int r = 0; r < kTiles; ++r) {
             const uint32_t tile = tile0 + r < Q.tiles ? tile0 + r : Q.tiles - 1;
-            B.codes[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(Q.codes) + (uint64_t(tile) * Q.blocks + block) * 64 + lane);
-#pragma unroll
-            for (int p = 0; p < kParts; ++p) {
-                const uint64_t at = (uint64_t(tile) * Q.groups + group + p) * 16;
-                B.scales[r][p] = *reinterpret_cast<const f16x4 *>(Q.scales + at + 4 * g);
-                if constexpr (kZeros) B.zeros[r][p] = Q.zeros[at + n];
-            }
-        }
-        const uint16_t *from = x + int64_t(block) * 128;
-        if (block < last || Q.cols % 128 == 0) {
-            typedef u32x4 u32x4_any __attribute__((aligned(2)));
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                B.x[j] = kAligned ? *reinterpret_cast<const u32x4 *>(from + 32 * j) : *reinterpret_cast<const u32x4_any *>(from + 32 * j);
-        } else {  // zeros past the last column
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const int64_t c = int64_t(block) * 128 + 32 * j + 8 * g + e;
-                    const uint32_t a = c < Q.cols ? from[32 * j + e] : 0, z = c + 1 < Q.cols ? from[32 * j + e + 1] : 0;
-                    B.x[j][e / 2] = a | z << 16;
-                }
-        }
-    };
-    f32x4 total[kTiles];
-#pragma unroll
-    for (int r = 0; r < kTiles; ++r) total[r] = f32x4{0, 0, 0, 0};
-    auto add = [&](const Block &B) {
-#pragma unroll
-        for (int r = 0; r < kTiles; ++r)
-#pragma unroll
-            for (int p = 0; p < kParts; ++p) {
-                const Zero<kBf16> zero(kZeros ? static_cast<float>(B.zeros[r][p]) : 8.0f);
-                f32x4 sum = {0, 0, 0, 0};
-#pragma unroll
-                for (int j = 4 / kParts * p; j < 4 / kParts * (p + 1); ++j) sum = product<kBf16>(zero.operand(B.codes[r][j]), B.x[j], sum);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) total[r][i] += sum[i] * static_cast<float>(B.scales[r][p][i]);
-            }
-    };
-    if (wave < Q.blocks) {
-        Block a, z;
-        uint32_t block = wave;
-        load(block, a);
-        for (;;) {
-            const uint32_t second = block + waves, third = second + waves;
-            load(second < last ? second : last, z);
-            add(a);
-            if (second >= Q.blocks) break;
-            load(third < last ? third : last, a);
-            add(z);
-            if (third >= Q.blocks) break;
-            block = third;
+            codes[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(Q.codes) + (uint64_t(tile) * Q.blocks + block) * 64 +
+                                                  (wanted <= last ? lane : 0));
+            const uint64_t at = (uint64_t(tile) * Q.groups + group) * 16;
+            scales[r] = *reinterpret_cast<const Scales<kParts> *>(Q.scales + at + 4 * kParts * g);
+            if constexpr (kZeros) zeros[r] = *reinterpret_cast<const Bytes<kParts> *>(Q.zeros + at + kParts * n);
         }
     }
+};
+
+// total += the block's products with x, the operands of its four instructions.
+template <int kTiles, int kParts, bool kZeros, bool kBf16>
+__device__ __forceinline__ void add_block(f32x4 (&total)[kTiles], const Block<kTiles, kParts, kZeros> &B, const u32x4 (&x)[4]) {
+#pragma unroll
+    for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) {
+            const Operand<kBf16, kZeros> operand(kZeros ? static_cast<float>(B.zeros[r] >> (8 * p) & 0xffu) : 8.0f);
+            f32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+            for (int j = 4 / kParts * p; j < 4 / kParts * (p + 1); ++j) sum = product<kBf16>(operand.of(B.codes[r][j]), x[j], sum);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) total[r][i] += sum[i] * (static_cast<float>(B.scales[r][4 * p + i]) * Operand<kBf16, kZeros>::kUnit);
+        }
+}
+
+// The waves' sums are added in their order; a lane has rows 4g + 0..3 of every tile for the right-hand side of its column.
+template <int kTiles>
+__device__ __forceinline__ void join_waves(const Q4Params &Q, float *s_part, uint32_t tile0, const f32x4 (&total)[kTiles]) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, n = lane & 15, g = lane >> 4;
     if (n < Q.nb)
 #pragma unroll
         for (int r = 0; r < kTiles; ++r) *reinterpret_cast<f32x4 *>(s_part + ((wave * Q.nb + n) * kTiles + r) * 16 + 4 * g) = total[r];
@@ -251,45 +265,144 @@ __global__ __launch_bounds__(512) void endor_q4_gemm_kernel(Q4Params Q) {
         for (uint32_t w = 0; w < waves; ++w) sum += s_part[w * Q.nb * kTiles * 16 + i];
         const uint32_t b = i / (kTiles * 16);
         const int64_t row = int64_t(tile0) * 16 + i % (kTiles * 16);
-        if (row < Q.rows) Q.y[b * Q.rows + row] = sum;
+        if (row < Q.rows) (Q.splits > 1 ? Q.partial + int64_t(blockIdx.y) * Q.nb * Q.rows : Q.y)[b * Q.rows + row] = sum;
     }
 }
 
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+// Elements c to c + 7 of a vector of x, zeros past the last column.
+__device__ __forceinline__ u32x4 columns_of(const uint16_t *x, int64_t c, int64_t cols) {
+    if (c + 8 <= cols) return *reinterpret_cast<const u32x4_any *>(x + c);
+    u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (c + e < cols) v[e / 2] |= uint32_t(x[c + e]) << (16 * (e & 1));
+    return v;
+}
+
+// Few right-hand sides: all of x lies in LDS, in the order of the operands, [block][32 columns][quarter][right-hand side][8 columns].
+// A workgroup has one row tile, its waves take the blocks in turn, kDepth of them on their way.
+template <int kDepth, int kParts, bool kZeros, bool kBf16>
+__global__ __launch_bounds__(1024) void endor_q4_gemv_kernel(Q4Params Q) {
+    extern __shared__ u32x4 s_x[];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, n = lane & 15, g = lane >> 4;
+    const uint32_t first = blockIdx.y * Q.per_split, end = first + Q.per_split < Q.blocks ? first + Q.per_split : Q.blocks;
+    const uint32_t units = (end - first) * 16 * Q.nb, column = n < Q.nb ? n : Q.nb - 1;  // columns past the last right-hand side are not stored
+    for (uint32_t u = threadIdx.x; u < units; u += blockDim.x)
+        s_x[u] = columns_of(Q.x + int64_t(u % Q.nb) * Q.ldx, int64_t(first) * 128 + u / Q.nb * 8, Q.cols);
+    Block<1, kParts, kZeros> ring[kDepth];
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) ring[d].load(Q, blockIdx.x, first + wave + d * waves, end - 1, lane);
+    // a barrier for LDS alone: the blocks on their way are not waited for
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    f32x4 total[1] = {{0, 0, 0, 0}};
+    for (uint32_t block = first + wave; block < end; block += kDepth * waves) {
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d) {
+            const uint32_t at = block + d * waves;
+            if (at >= end) break;
+            u32x4 x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = s_x[(((at - first) * 4 + j) * 4 + g) * Q.nb + column];
+            add_block<1, kParts, kZeros, kBf16>(total, ring[d], x);
+            ring[d].load(Q, blockIdx.x, at + kDepth * waves, end - 1, lane);
+        }
+    }
+    __syncthreads();
+    join_waves<1>(Q, reinterpret_cast<float *>(s_x), blockIdx.x, total);
+}
+
+// More right-hand sides: x comes from the caches, once for kTiles row tiles.
 template <int kTiles, int kParts, bool kZeros, bool kBf16>
-void launch_aligned(const Q4Params &Q, uint32_t waves, hipStream_t s) {
-    const bool even = (reinterpret_cast<uintptr_t>(Q.x) & 15) == 0 && (Q.ldx % 8 == 0 || Q.nb == 1);
-    hipLaunchKernelGGL((even ? endor_q4_gemm_kernel<kTiles, kParts, kZeros, kBf16, true> : endor_q4_gemm_kernel<kTiles, kParts, kZeros, kBf16, false>),
-                       dim3((Q.tiles + kTiles - 1) / kTiles), dim3(64 * waves), waves * Q.nb * kTiles * 16 * sizeof(float), s, Q);
+__global__ __launch_bounds__(512) void endor_q4_gemm_kernel(Q4Params Q) {
+    extern __shared__ float s_part[];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, n = lane & 15, g = lane >> 4;
+    const uint32_t first = blockIdx.y * Q.per_split, end = first + Q.per_split < Q.blocks ? first + Q.per_split : Q.blocks;
+    const uint32_t tile0 = blockIdx.x * kTiles, last = end - 1;
+    const uint16_t *row = Q.x + int64_t(n < Q.nb ? n : Q.nb - 1) * Q.ldx;  // columns past the last right-hand side are not stored
+    struct {
+        Block<kTiles, kParts, kZeros> w;
+        u32x4 x[4];
+    } held;
+    auto load = [&](uint32_t wanted) {
+        held.w.load(Q, tile0, wanted, last, lane);
+        const uint32_t block = wanted < last ? wanted : last;
+        const int64_t c = int64_t(block) * 128 + 8 * g;
+        if (block < Q.blocks - 1 || Q.cols % 128 == 0) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) held.x[j] = *reinterpret_cast<const u32x4_any *>(row + c + 32 * j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) held.x[j] = columns_of(row, c + 32 * j, Q.cols);
+        }
+    };
+    f32x4 total[kTiles];
+#pragma unroll
+    for (int r = 0; r < kTiles; ++r) total[r] = f32x4{0, 0, 0, 0};
+    load(first + wave);
+    for (uint32_t block = first + wave; block < end; block += waves) {
+        add_block<kTiles, kParts, kZeros, kBf16>(total, held.w, held.x);
+        load(block + waves);
+    }
+    join_waves<kTiles>(Q, s_part, tile0, total);
 }
-template <int kTiles, int kParts>
-void launch_kind(const Q4Params &Q, bool bf16, uint32_t waves, hipStream_t s) {
+
+__global__ __launch_bounds__(256) void endor_q4_join_kernel(const float *partial, float *y, int64_t count, uint32_t splits) {
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= count) return;
+    float sum = 0;
+    for (uint32_t s = 0; s < splits; ++s) sum += partial[s * count + i];
+    y[i] = sum;
+}
+
+template <int kParts, bool kZeros, bool kBf16>
+void launch(const Q4Params &Q, const Plan &p, hipStream_t s) {
+    const uint32_t tiles = p.tiles ? p.tiles : 1;
+    size_t lds = size_t(p.waves) * Q.nb * tiles * 16 * sizeof(float);
+    if (!p.tiles && lds < endor_q4_plan::x_bytes(p.per_split, Q.nb)) lds = endor_q4_plan::x_bytes(p.per_split, Q.nb);
+    const auto kernel = p.tiles == 4   ? endor_q4_gemm_kernel<4, kParts, kZeros, kBf16>
+                        : p.tiles == 2 ? endor_q4_gemm_kernel<2, kParts, kZeros, kBf16>
+                        : p.tiles == 1 ? endor_q4_gemm_kernel<1, kParts, kZeros, kBf16>
+                        : p.depth == 2 ? endor_q4_gemv_kernel<2, kParts, kZeros, kBf16>
+                                       : endor_q4_gemv_kernel<1, kParts, kZeros, kBf16>;
+    hipLaunchKernelGGL(kernel, dim3((Q.tiles + tiles - 1) / tiles, p.splits), dim3(64 * p.waves), lds, s, Q);
+}
+template <int kParts>
+void launch_kind(const Q4Params &Q, const Plan &p, bool bf16, hipStream_t s) {
     if (Q.zeros)
-        bf16 ? launch_aligned<kTiles, kParts, true, true>(Q, waves, s) : launch_aligned<kTiles, kParts, true, false>(Q, waves, s);
+        bf16 ? launch<kParts, true, true>(Q, p, s) : launch<kParts, true, false>(Q, p, s);
     else
-        bf16 ? launch_aligned<kTiles, kParts, false, true>(Q, waves, s) : launch_aligned<kTiles, kParts, false, false>(Q, waves, s);
+        bf16 ? launch<kParts, false, true>(Q, p, s) : launch<kParts, false, false>(Q, p, s);
 }
-template <int kTiles>
-void launch_parts(const Q4Params &Q, int group, bool bf16, uint32_t waves, hipStream_t s) {
+void launch_group(Q4Params Q, const Plan &p, int group, bool bf16, hipStream_t s) {
+    Q.splits = p.splits;
+    Q.per_split = p.per_split;
     if (group == 32)
-        launch_kind<kTiles, 4>(Q, bf16, waves, s);
+        launch_kind<4>(Q, p, bf16, s);
     else if (group == 64)
-        launch_kind<kTiles, 2>(Q, bf16, waves, s);
+        launch_kind<2>(Q, p, bf16, s);
     else
-        launch_kind<kTiles, 1>(Q, bf16, waves, s);
-}
-void launch(const Q4Params &Q, int group, bool bf16, int tiles, uint32_t waves, hipStream_t s) {
-    if (tiles == 4)
-        launch_parts<4>(Q, group, bf16, waves, s);
-    else if (tiles == 2)
-        launch_parts<2>(Q, group, bf16, waves, s);
-    else
-        launch_parts<1>(Q, group, bf16, waves, s);
+        launch_kind<1>(Q, p, bf16, s);
+    if (p.splits > 1) {
+        const int64_t count = Q.rows * Q.nb;
+        hipLaunchKernelGGL(endor_q4_join_kernel, dim3(static_cast<uint32_t>((count + 255) / 256)), dim3(256), 0, s, Q.partial, Q.y, count, p.splits);
+    }
 }
 
 }  // namespace
 
 extern "C" size_t endor_q4_bytes(int64_t rows, int64_t cols, int group, int with_zeros) {
     return sizes_ok(rows, cols, group) ? layout_of(rows, cols, group, with_zeros != 0).bytes : 0;
+}
+
+extern "C" size_t endor_q4_scratch_bytes(int64_t rows, int64_t cols, int group, int nb) {
+    if (!sizes_ok(rows, cols, group) || nb < 1 || nb > ENDOR_GEMM_MAX_BATCH || rows == 0 || cols == 0) return 0;
+    const Layout l = layout_of(rows, cols, group, false);
+    const Plan p = make_plan(static_cast<uint32_t>(l.tiles), static_cast<uint32_t>(l.blocks), static_cast<uint32_t>(nb));
+    return p.splits > 1 ? (size_t(p.splits) * nb * rows * sizeof(float) + 255) & ~size_t(255) : 0;
 }
 
 extern "C" endor_status endor_q4_pack(int64_t rows, int64_t cols, int group, const uint8_t *d_codes, const uint16_t *d_scales,
@@ -337,13 +450,15 @@ extern "C" endor_status endor_q4_quantize(int64_t rows, int64_t cols, int group,
     return ENDOR_OK;
 }
 
+namespace {
 __global__ __launch_bounds__(256) void endor_q4_zero_kernel(float *y, int64_t count) {
     const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (i < count) y[i] = 0.0f;
 }
+}  // namespace
 
 extern "C" endor_status endor_q4_gemm(int64_t rows, int64_t cols, int group, int with_zeros, const void *d_packed, size_t packed_bytes, int dtype,
-                                      const void *d_x, int64_t ldx, int nb, float *d_y, void *stream) {
+                                      const void *d_x, int64_t ldx, int nb, float *d_y, void *d_scratch, size_t scratch_bytes, void *stream) {
     if (rows < 0 || cols < 0 || nb < 0 || nb > ENDOR_GEMM_MAX_BATCH) return ENDOR_ERR_INVALID_ARG;
     if (!sizes_ok(rows, cols, group) || (dtype != ENDOR_F16 && dtype != ENDOR_BF16)) return ENDOR_ERR_UNSUPPORTED;
     if (rows == 0 || nb == 0) return ENDOR_OK;
@@ -370,6 +485,12 @@ extern "C" endor_status endor_q4_gemm(int64_t rows, int64_t cols, int group, int
     Q.groups = static_cast<uint32_t>(l.groups);
     Q.per_group_shift = group > 128 ? static_cast<uint32_t>(__builtin_ctz(static_cast<unsigned>(group))) - 7 : 0;
     Q.nb = static_cast<uint32_t>(nb);
-    launch(Q, group, dtype == ENDOR_BF16, l.tiles >= 1024 ? 2 : 1, 8, s);
+    const Plan p = make_plan(Q.tiles, Q.blocks, Q.nb);
+    if (p.splits > 1) {
+        if (!aligned(d_scratch, 256)) return ENDOR_ERR_INVALID_ARG;
+        if (scratch_bytes < endor_q4_scratch_bytes(rows, cols, group, nb)) return ENDOR_ERR_BUFFER_TOO_SMALL;
+        Q.partial = static_cast<float *>(d_scratch);
+    }
+    launch_group(Q, p, group, dtype == ENDOR_BF16, s);
     return hipGetLastError() == hipSuccess ? ENDOR_OK : ENDOR_ERR_HIP;
 }

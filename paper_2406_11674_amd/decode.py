@@ -8,7 +8,7 @@ from dataclasses import dataclass
 from . import binding
 from .binding import _check, _dptr, _i64, _p, _stream_handle, _sz, _torch
 
-__all__ = ["KVCache", "kv_append", "attn_decode", "kv_evict", "Q4Matrix", "q4_pack", "q4_quantize", "q4_gemm"]
+__all__ = ["KVCache", "kv_append", "attn_decode", "kv_evict", "Q4Matrix", "q4_pack", "q4_quantize", "q4_scratch_bytes", "q4_gemm"]
 
 _i32 = ctypes.c_int32
 
@@ -37,7 +37,9 @@ def _lib():
         L.endor_q4_bytes.argtypes = [_i64, _i64, ctypes.c_int, ctypes.c_int]
         L.endor_q4_pack.argtypes = [_i64, _i64, ctypes.c_int, _p, _p, _p, _p, _sz, _p]
         L.endor_q4_quantize.argtypes = [_i64, _i64, ctypes.c_int, _p, _p, _p, _p, _p]
-        L.endor_q4_gemm.argtypes = [_i64, _i64, ctypes.c_int, ctypes.c_int, _p, _sz, ctypes.c_int, _p, _i64, ctypes.c_int, _p, _p]
+        L.endor_q4_scratch_bytes.restype = _sz
+        L.endor_q4_scratch_bytes.argtypes = [_i64, _i64, ctypes.c_int, ctypes.c_int]
+        L.endor_q4_gemm.argtypes = [_i64, _i64, ctypes.c_int, ctypes.c_int, _p, _sz, ctypes.c_int, _p, _i64, ctypes.c_int, _p, _p, _sz, _p]
         _declared = L
     return L
 
@@ -264,7 +266,12 @@ def q4_quantize(dense, group=128, zeros=False, stream=None):
     return codes, scales, points
 
 
-def q4_gemm(m, X, Y=None, stream=None):
+def q4_scratch_bytes(m, nb):
+    """endor_q4_scratch_bytes: scratch of q4_gemm with that many right-hand sides; mostly none."""
+    return int(_lib().endor_q4_scratch_bytes(m.rows, m.cols, m.group, nb))
+
+
+def q4_gemm(m, X, Y=None, scratch=None, stream=None):
     """endor_q4_gemm: Y (fp32, nb x rows) = X W^T; X: (nb, cols) float16 or bfloat16 (row stride = ldx), nb <= 16."""
     torch = _torch()
     if X.dim() != 2 or X.shape[1] != m.cols or (m.cols > 1 and X.stride(1) != 1):
@@ -274,8 +281,13 @@ def q4_gemm(m, X, Y=None, stream=None):
         Y = torch.empty((nb, m.rows), dtype=torch.float32, device=X.device)
     elif Y.dtype != torch.float32 or Y.numel() != nb * m.rows or not Y.is_contiguous():
         raise ValueError("Y must be a contiguous fp32 tensor of nb*rows elements")
-    _on(m.packed.get_device(), X, Y)
+    L = _lib()
+    if scratch is None:
+        need = L.endor_q4_scratch_bytes(m.rows, m.cols, m.group, nb)
+        if need:
+            scratch = torch.empty(need, dtype=torch.uint8, device=X.device)
+    _on(m.packed.get_device(), X, Y, scratch)
     ldx = X.stride(0) if nb > 1 else m.cols
-    _check(_lib().endor_q4_gemm(m.rows, m.cols, m.group, m.zeros, _dptr(m.packed), m.packed.numel(), _dtype_code(X.dtype), _dptr(X), ldx, nb,
-                                _dptr(Y), _stream_handle(stream)), "endor_q4_gemm")
+    _check(L.endor_q4_gemm(m.rows, m.cols, m.group, m.zeros, _dptr(m.packed), m.packed.numel(), _dtype_code(X.dtype), _dptr(X), ldx, nb,
+                           _dptr(Y), _dptr(scratch), 0 if scratch is None else scratch.numel(), _stream_handle(stream)), "endor_q4_gemm")
     return Y

@@ -84,14 +84,20 @@ def test_q4():
         assert L.endor_q4_bytes(rows, cols, group, 0) == 0
     size = L.endor_q4_bytes(16, 128, 32, 0)
 
-    def gemm(rows=16, cols=128, group=32, zeros=0, packed=FAKE, nbytes=size, dtype=0, x=FAKE, ldx=128, nb=2, y=FAKE):
-        return L.endor_q4_gemm(rows, cols, group, zeros, packed, nbytes, dtype, x, ldx, nb, y, None)
+    def gemm(rows=16, cols=128, group=32, zeros=0, packed=FAKE, nbytes=size, dtype=0, x=FAKE, ldx=128, nb=2, y=FAKE, scratch=None, room=0):
+        return L.endor_q4_gemm(rows, cols, group, zeros, packed, nbytes, dtype, x, ldx, nb, y, scratch, room, None)
 
     for kw, status in ((dict(rows=-1), 1), (dict(cols=-1), 1), (dict(nb=-1), 1), (dict(nb=17), 1), (dict(group=33), 3), (dict(dtype=2), 3), (dict(packed=None), 1),
                        (dict(packed=FAKE + 128), 1), (dict(nbytes=size - 1), 2), (dict(zeros=1, nbytes=0), 2), (dict(x=None), 1), (dict(x=FAKE + 1), 1),
                        (dict(ldx=127), 1), (dict(y=None), 1), (dict(y=FAKE + 2), 1), (dict(rows=1 << 20, cols=1 << 20), 3)):
         assert gemm(**kw) == status, kw
     assert gemm(rows=0) == 0 and gemm(nb=0) == 0
+    wide = dict(rows=16, cols=100000, group=128, ldx=100000, nbytes=1 << 30)  # its columns are split, which takes scratch
+    need = L.endor_q4_scratch_bytes(16, 100000, 128, 2)
+    assert need > 0 and need % 256 == 0 and L.endor_q4_scratch_bytes(16, 128, 32, 2) == 0
+    assert gemm(**wide) == 1 and gemm(scratch=FAKE + 8, room=need, **wide) == 1 and gemm(scratch=FAKE, room=need - 1, **wide) == 2
+    for args in ((-1, 8, 32, 1), (16, 100000, 33, 1), (16, 100000, 128, 0), (16, 100000, 128, 17)):
+        assert L.endor_q4_scratch_bytes(*args) == 0
     assert L.endor_q4_pack(16, 128, 32, None, FAKE, None, FAKE, size, None) == 1
     assert L.endor_q4_pack(16, 128, 32, FAKE, FAKE + 1, None, FAKE, size, None) == 1
     assert L.endor_q4_pack(16, 128, 32, FAKE, FAKE, None, FAKE + 8, size, None) == 1

@@ -57,7 +57,7 @@ def test_every_batch(nb):
         check(m, w, x)
 
 
-@pytest.mark.parametrize("shape", [(1024, 8192), (8192, 1024), (20000, 512), (40, 28672), (4100, 3001)], ids=str)
+@pytest.mark.parametrize("shape", [(1024, 8192), (8192, 1024), (20000, 512), (40, 28672), (4100, 3001), (1500, 20000), (2047, 9001), (17, 70001), (13000, 1600)], ids=str)
 def test_larger(shape):
     print("q4", shape, flush=True)
     rows, cols = shape
