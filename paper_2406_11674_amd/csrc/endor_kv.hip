@@ -11,6 +11,7 @@ namespace {
 
 using endor_device::u32x4;
 using endor_device::wave_inclusive_scan;
+using endor_device::wave_sum;
 using endor_kv::aligned;
 using endor_kv::Cache;
 using endor_kv::capacity_of;
@@ -18,6 +19,9 @@ using endor_kv::clamp_length;
 using endor_kv::page_of;
 using endor_kv::read_cache;
 using endor_kv::slot_at;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------- append
 
@@ -32,36 +36,83 @@ struct AppendParams {
     int32_t tokens, capacity;
 };
 
-// One workgroup per sequence and token; a separate launch advances the lengths behind it.
-__global__ __launch_bounds__(256) void endor_kv_append_kernel(AppendParams A) {
-    const uint32_t b = blockIdx.y, t = blockIdx.x;
-    const int32_t length = clamp_length(A.lengths[b], A.capacity);
-    const int32_t count = A.counts ? clamp_length(A.counts[b], A.tokens) : A.tokens;
-    if (static_cast<int32_t>(t) >= count || length + int64_t(t) >= A.capacity) return;
-    const uint32_t slot = length + t, heads = A.C.kv_heads, dim = A.C.dim;
-    uint32_t page;
-    if (page_of(A.C, A.C.pages + b * A.C.pages_stride, slot, &page)) {
-        for (uint32_t i = threadIdx.x; i < heads * dim; i += 256) {
-            const uint32_t h = i / dim, d = i % dim;
-            const int64_t from = int64_t(b) * A.seq_stride + int64_t(t) * A.token_stride + int64_t(h) * A.head_stride + d;
-            const int64_t to = slot_at(A.C, page, h, slot) + d;
-            A.C.k[to] = A.k[from];
-            A.C.v[to] = A.v[from];
+// Tokens first to first + count of heads head0 to head0 + heads of a sequence.  Threads: x the 16-byte units of a head's key or value, y the
+// keys and then the values of the heads and on to the next token, four of them on their way.
+__device__ __forceinline__ void store_tokens(const AppendParams &A, uint32_t b, uint32_t head0, uint32_t heads, uint32_t length, uint32_t seen,
+                                             uint32_t first, uint32_t count) {
+    typedef u32x4 u32x4_any __attribute__((aligned(2)));
+    const uint32_t rows = 2 * heads, d = 8 * threadIdx.x;
+    const int32_t *table = A.C.pages + int64_t(b) * A.C.pages_stride;
+    uint32_t t = first, r = threadIdx.y;
+    auto settle = [&] {
+        while (r >= rows) {
+            r -= rows;
+            ++t;
         }
+    };
+    settle();
+    while (t < first + count) {
+        u32x4 held[4];
+        uint16_t *dst[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            dst[k] = nullptr;
+            uint32_t page;
+            if (t < first + count && page_of(A.C, table, length + t, &page)) {
+                const uint32_t h = head0 + (r < heads ? r : r - heads);
+                held[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any *>(
+                    (r < heads ? A.k : A.v) + int64_t(b) * A.seq_stride + int64_t(t) * A.token_stride + int64_t(h) * A.head_stride + d));
+                dst[k] = (r < heads ? A.C.k : A.C.v) + slot_at(A.C, page, h, length + t) + d;
+            }
+            r += blockDim.y;
+            settle();
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (dst[k]) *reinterpret_cast<u32x4 *>(dst[k]) = held[k];
     }
-    for (uint32_t h = threadIdx.x; h < heads; h += 256) {
-        const int64_t at = (int64_t(b) * heads + h) * A.capacity + slot;
-        if (A.weights) A.weights[at] = 0.0f;
-        if (A.positions) A.positions[at] = A.seen[b] + static_cast<int32_t>(t);
+    const uint32_t thread = threadIdx.y * blockDim.x + threadIdx.x, threads = blockDim.x * blockDim.y;
+    if (A.weights || A.positions)
+        for (uint32_t i = thread; i < heads * count; i += threads) {
+            const uint32_t at = first + i % count;
+            const int64_t to = (int64_t(b) * A.C.kv_heads + head0 + i / count) * A.capacity + length + at;
+            if (A.weights) A.weights[to] = 0.0f;
+            if (A.positions) A.positions[to] = static_cast<int32_t>(seen + at);
+        }
+}
+
+// How many tokens of the sequence are stored.
+__device__ __forceinline__ uint32_t stored_of(const AppendParams &A, uint32_t b, uint32_t length) {
+    const uint32_t count = A.counts ? clamp_length(A.counts[b], A.tokens) : A.tokens, room = A.capacity - length;
+    return count < room ? count : room;
+}
+
+// A few tokens: one workgroup per sequence, which also advances its length.
+__global__ __launch_bounds__(1024) void endor_kv_append_kernel(AppendParams A) {
+    const uint32_t b = blockIdx.x, length = clamp_length(A.lengths[b], A.capacity), seen = A.seen[b], stored = stored_of(A, b, length);
+    if (stored) store_tokens(A, b, 0, A.C.kv_heads, length, seen, 0, stored);
+    __syncthreads();  // the lengths may be changed in place
+    if (threadIdx.x == 0 && threadIdx.y == 0) {
+        A.lengths_out[b] = length + stored;
+        A.seen_out[b] = seen + stored;
     }
+}
+
+constexpr uint32_t kTokensEach = 8;
+
+// Prompts: kTokensEach tokens of a few heads a workgroup, so that a thread has four units of a head's; a second launch advances the lengths.
+__global__ __launch_bounds__(256) void endor_kv_append_many_kernel(AppendParams A, uint32_t heads_each) {
+    const uint32_t b = blockIdx.z, first = blockIdx.x * kTokensEach, head0 = blockIdx.y * heads_each;
+    const uint32_t length = clamp_length(A.lengths[b], A.capacity), stored = stored_of(A, b, length), heads = A.C.kv_heads;
+    if (first < stored)
+        store_tokens(A, b, head0, heads - head0 < heads_each ? heads - head0 : heads_each, length, A.seen[b], first,
+                     stored - first < kTokensEach ? stored - first : kTokensEach);
 }
 
 __global__ __launch_bounds__(256) void endor_kv_advance_kernel(AppendParams A) {
     const int32_t b = blockIdx.x * 256 + threadIdx.x;
     if (b >= A.C.batch) return;
-    const int32_t length = clamp_length(A.lengths[b], A.capacity);
-    const int32_t count = A.counts ? clamp_length(A.counts[b], A.tokens) : A.tokens;
-    const int32_t stored = count < A.capacity - length ? count : A.capacity - length;
+    const uint32_t length = clamp_length(A.lengths[b], A.capacity), stored = stored_of(A, b, length);
     A.lengths_out[b] = length + stored;
     A.seen_out[b] = A.seen[b] + stored;
 }
@@ -88,117 +139,306 @@ __device__ __forceinline__ uint32_t key_of(float w, int32_t position, int64_t ne
     return bits >> 31 ? ~bits : bits | 0x80000000u;
 }
 
-constexpr int kSelectThreads = 1024;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kBinBits = 11, kBins = 1 << kBinBits;  // of a pass over the keys
+static_assert(kBins == 2 * kSelectThreads, "a thread reads two bins");
 
-// Sum over the workgroup; every thread gets it.
-__device__ __forceinline__ uint32_t group_sum(uint32_t x, uint32_t *s_part) {
+struct SelectShared {
+    uint32_t bins[kBins];
+    uint32_t part[2][kSelectWaves];
+    uint32_t found[3];  // the bin that the last kept key is in, the keys above it, the keys in it
+};
+
+// Exclusive prefix over the workgroup, and the total.  `turn` changes from one call to the next, so that one barrier does.
+__device__ __forceinline__ uint32_t group_scan(uint32_t x, SelectShared &S, uint32_t turn, uint32_t *total) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t upto = wave_inclusive_scan(x);
-    __syncthreads();
-    if (lane == 63) s_part[wave] = upto;
-    __syncthreads();
-    uint32_t sum = 0;
-    for (int w = 0; w < kSelectThreads / 64; ++w) sum += s_part[w];
-    return sum;
-}
-// Exclusive prefix over the workgroup, and the total.
-__device__ __forceinline__ uint32_t group_scan(uint32_t x, uint32_t *s_part, uint32_t *total) {
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t upto = wave_inclusive_scan(x);
-    __syncthreads();
-    if (lane == 63) s_part[wave] = upto;
+    if (lane == 63) S.part[turn & 1][wave] = upto;
     __syncthreads();
     uint32_t before = 0, sum = 0;
-    for (uint32_t w = 0; w < kSelectThreads / 64; ++w) {
-        before += w < wave ? s_part[w] : 0;
-        sum += s_part[w];
+#pragma unroll
+    for (uint32_t w = 0; w < kSelectWaves; ++w) {
+        before += w < wave ? S.part[turn & 1][w] : 0;
+        sum += S.part[turn & 1][w];
     }
     *total = sum;
     return before + upto - x;
 }
 
-// One workgroup per sequence and kv head: the key of the budget-th largest, bit by bit; then the slots that come free below the
-// budget and the kept ones past it, in order.
+// A token's keys and values from one slot to another: 16 bytes a lane, K and V side by side.  `per`: units of a token.
+__device__ __forceinline__ void move_units(const Cache &C, const int32_t *table, uint32_t h, const int32_t *to, const int32_t *from, uint32_t first,
+                                           uint32_t count, uint32_t thread, uint32_t threads) {
+    const uint32_t half = C.dim / 8, per = 2 * half;
+    for (uint32_t u0 = thread; u0 < count * per; u0 += 4 * threads) {
+        u32x4 held[4];
+        uint16_t *dst[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t u = u0 + k * threads;
+            dst[k] = nullptr;
+            if (u < count * per) {
+                const uint32_t i = first + u / per, part = u % per, a = to[i], z = from[i];
+                uint32_t a_page, z_page;
+                if (page_of(C, table, a, &a_page) && page_of(C, table, z, &z_page)) {
+                    uint16_t *pool = part < half ? C.k : C.v;
+                    const uint32_t d = 8 * (part < half ? part : part - half);
+                    held[k] = *reinterpret_cast<const u32x4 *>(pool + slot_at(C, z_page, h, z) + d);
+                    dst[k] = pool + slot_at(C, a_page, h, a) + d;
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (dst[k]) *reinterpret_cast<u32x4 *>(dst[k]) = held[k];
+    }
+}
+
+// One workgroup per sequence and kv head finds the key of the last token that stays, then the slots that come free below the budget and the
+// kept ones past it, in order.
+//
+// The keys are looked at 11 bits at a time from the highest bit in which they differ: a histogram in LDS, and a scan of it from
+// the top, three passes at most.  (Weights of one row share most of their leading bits: a fixed first digit would have nearly
+// all keys in a few bins, where LDS adds them one after the other.)  A wave has a contiguous piece of the slots, 256 of them at a
+// time, four to a lane: loads are whole lines, and ranks in the order of slots need wave scans only.  kChunks: such chunks of a wave that it
+// keeps as keys in registers; 0: the keys are formed anew in every pass, for rows past 32768 slots.
+// kMove: the moves are few and done here.
+template <int kChunks, bool kMove>
 __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictParams E) {
-    __shared__ uint32_t s_part[kSelectThreads / 64];
+    __shared__ SelectShared S;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t b = blockIdx.y, h = blockIdx.x;
     const int64_t row = int64_t(b) * E.C.kv_heads + h, base = row * E.capacity;
     const float *w = E.weights + base;
     const int32_t *pos = E.positions + base;
     float *w_out = E.weights_out + base;
     int32_t *pos_out = E.positions_out + base;
-    const int32_t length = clamp_length(E.lengths[b], E.most_len), budget = E.budget;
-    if (length <= budget) {
-        for (int32_t t = threadIdx.x; t < length; t += kSelectThreads) {
-            w_out[t] = w[t];
-            pos_out[t] = pos[t];
-        }
-        if (threadIdx.x == 0) E.count[row] = 0;
+    const uint32_t length = clamp_length(E.lengths[b], E.most_len), budget = E.budget;
+    const bool copies = w_out != w || pos_out != pos;  // what stays where it is has to be written
+    if (E.lengths_out != E.lengths && h == 0 && threadIdx.x == 0) E.lengths_out[b] = length < budget ? length : budget;
+    if (length <= budget || budget == 0) {
+        const uint32_t kept = length < budget ? length : budget;
+        if (copies)
+            for (uint32_t t = threadIdx.x; t < kept; t += kSelectThreads) {
+                w_out[t] = w[t];
+                pos_out[t] = pos[t];
+            }
+        if (!kMove && threadIdx.x == 0) E.count[row] = 0;
         return;
     }
     const int64_t newest = int64_t(E.seen[b]) - E.recent;
-    // the largest threshold that at least `budget` keys reach
-    uint32_t least = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t trial = least | (1u << bit);
-        uint32_t n = 0;
-        for (int32_t t = threadIdx.x; t < length; t += kSelectThreads) n += key_of(w[t], pos[t], newest) >= trial;
-        if (group_sum(n, s_part) >= static_cast<uint32_t>(budget)) least = trial;
+    const uint32_t chunks = kChunks ? kChunks : (length + 256 * kSelectWaves - 1) / (256 * kSelectWaves);
+    const uint32_t mine = wave * chunks * 256 + 4 * lane;  // slot of this lane's first key
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    typedef i32x4 i32x4_any __attribute__((aligned(4)));
+    constexpr uint32_t kStay = 0xffffffffu;
+    // Four keys from slot t on; of a slot past the length, 0.
+    auto keys_at = [&](uint32_t t) {
+        u32x4 key = {0, 0, 0, 0};
+        if (t + 4 <= length) {
+            const f32x4 x = *reinterpret_cast<const f32x4_any *>(w + t);
+            const i32x4 p = *reinterpret_cast<const i32x4_any *>(pos + t);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) key[e] = key_of(x[e], p[e], newest);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (t + e < length) key[e] = key_of(w[t + e], pos[t + e], newest);
+        }
+        return key;
+    };
+    u32x4 held[kChunks ? kChunks : 1];
+    if constexpr (kChunks > 0)
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) held[i] = keys_at(mine + 256 * i);
+    // f(slot of four keys, the keys) for all of the lane's
+    auto each = [&](auto f) {
+        if constexpr (kChunks > 0) {
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i) f(mine + 256 * i, held[i]);
+        } else {
+            for (uint32_t i = 0; i < chunks; ++i) f(mine + 256 * i, keys_at(mine + 256 * i));
+        }
+    };
+
+    uint32_t turn = 0, total;
+    // What stays whatever it weighs; the least and the largest key of the others.
+    uint32_t staying = 0, low = kStay, high = 0;
+    each([&](uint32_t t, u32x4 key) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool in = t + e < length;
+            staying += in && key[e] == kStay;
+            if (in && key[e] != kStay) {
+                low = key[e] < low ? key[e] : low;
+                high = key[e] > high ? key[e] : high;
+            }
+        }
+    });
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        const uint32_t l = __shfl_xor(low, d), u = __shfl_xor(high, d);
+        low = l < low ? l : low;
+        high = u > high ? u : high;
     }
-    uint32_t above = 0;
-    for (int32_t t = threadIdx.x; t < length; t += kSelectThreads) above += key_of(w[t], pos[t], newest) > least;
-    uint32_t ties = budget - group_sum(above, s_part);  // of the keys equal to `least`, the first so many stay
-    int32_t *holes = E.holes + row * E.most, *movers = E.movers + row * E.most;
-    uint32_t nholes = 0, nmovers = 0;
-    for (int32_t t0 = 0; t0 < length; t0 += kSelectThreads) {
-        const int32_t t = t0 + threadIdx.x;
-        const uint32_t key = t < length ? key_of(w[t], pos[t], newest) : 0;
-        uint32_t total;
-        const uint32_t tie = t < length && key == least;
-        const uint32_t rank = group_scan(tie, s_part, &total);
-        const bool keep = t < length && (key > least || (tie && rank < ties));
-        ties -= total < ties ? total : ties;
-        const uint32_t hole = t < budget && !keep, mover = t >= budget && keep;
-        const uint32_t before = group_scan(hole | mover << 16, s_part, &total);  // at most 1024 of each
-        if (hole) holes[nholes + (before & 0xffffu)] = t;
-        if (mover) movers[nmovers + (before >> 16)] = t;
-        nholes += total & 0xffffu;
-        nmovers += total >> 16;
-        if (t < budget && keep) {
-            w_out[t] = w[t];
-            pos_out[t] = pos[t];
+    if (lane == 0) {
+        S.bins[2 * wave] = low;
+        S.bins[2 * wave + 1] = high;
+    }
+    group_scan(staying, S, turn++, &total);  // its barrier is for both
+    staying = total;
+#pragma unroll
+    for (int v = 0; v < kSelectWaves; ++v) {
+        low = S.bins[2 * v] < low ? S.bins[2 * v] : low;
+        high = S.bins[2 * v + 1] > high ? S.bins[2 * v + 1] : high;
+    }
+    uint32_t least = kStay, ties = budget;  // keys above `least` stay, and the first `ties` of those equal to it
+    if (staying < budget) {
+        uint32_t need = budget - staying;
+        // more keys are left than are needed, so low <= high
+        const uint32_t range = high - low;
+        uint32_t shift = range >> kBinBits ? 32 - __clz(range) - kBinBits : 0;
+        uint64_t width = uint64_t(range) + 1;  // keys in [low, low + width) are still in question
+        for (;;) {
+            __syncthreads();  // the bins are not read any more
+            S.bins[threadIdx.x] = 0;
+            S.bins[threadIdx.x + kSelectThreads] = 0;
+            __syncthreads();
+            each([&](uint32_t t, u32x4 key) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (t + e < length && key[e] != kStay && key[e] >= low && key[e] - low < width) atomicAdd(&S.bins[(key[e] - low) >> shift], 1u);
+            });
+            __syncthreads();
+            const uint32_t top = kBins - 1 - 2 * threadIdx.x, c0 = S.bins[top], c1 = S.bins[top - 1];
+            const uint32_t above = group_scan(c0 + c1, S, turn++, &total);
+            if (above < need && above + c0 + c1 >= need) {
+                const bool second = above + c0 < need;
+                S.found[0] = second ? top - 1 : top;
+                S.found[1] = second ? above + c0 : above;
+                S.found[2] = second ? c1 : c0;
+            }
+            __syncthreads();
+            low += S.found[0] << shift;
+            need -= S.found[1];
+            if (shift == 0 || need == S.found[2]) {
+                least = low;
+                ties = shift == 0 ? need : 0xffffffffu;  // all of the bin stay: those from its lower end on
+                break;
+            }
+            width = uint64_t(1) << shift;
+            shift = shift > kBinBits ? shift - kBinBits : 0;
         }
     }
+
+    // Which stay: above, or equal and among the first.  Ties before this wave's, then before this lane's chunk by chunk.
+    uint32_t equal = 0;
+    each([&](uint32_t t, u32x4 key) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) equal += t + e < length && key[e] == least;
+    });
+    // Before the lane's first chunk: the waves before it.  (The scan's own lanes are counted chunk by chunk below.)
+    auto waves_before = [&](uint32_t x) {
+        uint32_t sum = wave_sum(x), before = 0;
+        if (lane == 0) S.part[turn & 1][wave] = sum;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t v = 0; v < kSelectWaves; ++v) before += v < wave ? S.part[turn & 1][v] : 0;
+        ++turn;
+        return before;
+    };
+    const uint32_t equal_before = waves_before(equal);
+    uint32_t ranked = equal_before, holes_mine = 0, movers_mine = 0;
+    // f(slot, bits of the four slots that stay) in order
+    auto each_kept = [&](auto f) {
+        ranked = equal_before;
+        each([&](uint32_t t, u32x4 key) {
+            uint32_t same = 0, more = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                same |= uint32_t(t + e < length && key[e] == least) << e;
+                more |= uint32_t(t + e < length && key[e] > least) << e;
+            }
+            const uint32_t upto = wave_inclusive_scan(__popc(same));
+            uint32_t rank = ranked + upto - __popc(same);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (same >> e & 1) more |= uint32_t(rank++ < ties) << e;
+            ranked += __builtin_amdgcn_readlane(upto, 63);
+            f(t, more);
+        });
+    };
+    // bits of the four slots from t on that lie below the budget, and below the length
+    auto below = [](uint32_t t, uint32_t end) { return t >= end ? 0u : end - t >= 4 ? 15u : (1u << (end - t)) - 1; };
+    each_kept([&](uint32_t t, uint32_t kept) {
+        holes_mine += __popc(below(t, budget) & ~kept);
+        movers_mine += __popc(kept & ~below(t, budget));
+    });
+    uint32_t holes = waves_before(holes_mine), movers = waves_before(movers_mine);
+    int32_t *hole_list = E.holes + row * E.most, *mover_list = E.movers + row * E.most;
+    each_kept([&](uint32_t t, uint32_t kept) {
+        const uint32_t free = below(t, budget) & ~kept, past = kept & ~below(t, budget);
+        const uint32_t f = wave_inclusive_scan(__popc(free)), m = wave_inclusive_scan(__popc(past));
+        uint32_t at = holes + f - __popc(free), to = movers + m - __popc(past);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (free >> e & 1) hole_list[at++] = t + e;
+            if (past >> e & 1) mover_list[to++] = t + e;
+            if (copies && (kept & below(t, budget)) >> e & 1) {
+                w_out[t + e] = w[t + e];
+                pos_out[t + e] = pos[t + e];
+            }
+        }
+        holes += __builtin_amdgcn_readlane(f, 63);
+        movers += __builtin_amdgcn_readlane(m, 63);
+    });
+    if (threadIdx.x == kSelectThreads - 1) S.found[0] = holes;
     __threadfence_block();
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < nholes; i += kSelectThreads) {
-        w_out[holes[i]] = w[movers[i]];
-        pos_out[holes[i]] = pos[movers[i]];
+    __syncthreads();  // the lists are whole, and nobody reads the slots that come free any more
+    const uint32_t count = S.found[0];
+    for (uint32_t i = threadIdx.x; i < count; i += kSelectThreads) {
+        const int32_t to = hole_list[i], from = mover_list[i];
+        w_out[to] = w[from];
+        pos_out[to] = pos[from];
     }
-    if (threadIdx.x == 0) E.count[row] = nholes;
+    if constexpr (kMove)
+        move_units(E.C, E.C.pages + b * E.C.pages_stride, h, hole_list, mover_list, 0, count, threadIdx.x, kSelectThreads);
+    else if (threadIdx.x == 0)
+        E.count[row] = count;
 }
 
-// Keys and values of the kept tokens past the budget; and the lengths.
+constexpr int kMovesEach = 32;  // of a workgroup of the move kernel
+
+// Keys and values of the kept tokens past the budget.
 __global__ __launch_bounds__(256) void endor_kv_move_kernel(EvictParams E) {
-    const uint32_t b = blockIdx.z, h = blockIdx.y;
+    const uint32_t b = blockIdx.z, h = blockIdx.y, first = blockIdx.x * kMovesEach;
     const int64_t row = int64_t(b) * E.C.kv_heads + h;
-    if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) {
-        const int32_t length = clamp_length(E.lengths[b], E.most_len);
-        E.lengths_out[b] = length < E.budget ? length : E.budget;
-    }
-    const int32_t count = E.count[row];
-    const int32_t *table = E.C.pages + b * E.C.pages_stride;
-    for (int32_t i = blockIdx.x; i < count; i += gridDim.x) {
-        const uint32_t to = E.holes[row * E.most + i], from = E.movers[row * E.most + i];
-        uint32_t to_page, from_page;
-        if (!page_of(E.C, table, to, &to_page) || !page_of(E.C, table, from, &from_page)) continue;
-        const int64_t dst = slot_at(E.C, to_page, h, to), src = slot_at(E.C, from_page, h, from);
-        for (int32_t d = threadIdx.x; d < E.C.dim; d += 256) {
-            E.C.k[dst + d] = E.C.k[src + d];
-            E.C.v[dst + d] = E.C.v[src + d];
-        }
-    }
+    const uint32_t count = E.count[row];
+    if (first >= count) return;
+    move_units(E.C, E.C.pages + b * E.C.pages_stride, h, E.holes + row * E.most, E.movers + row * E.most, first,
+               count - first < kMovesEach ? count - first : kMovesEach, threadIdx.x, 256);
 }
+
+// The lengths in place, once nobody reads the old ones any more.
+__global__ __launch_bounds__(256) void endor_kv_shorten_kernel(EvictParams E) {
+    const int32_t b = blockIdx.x * 256 + threadIdx.x;
+    if (b >= E.C.batch) return;
+    const int32_t length = clamp_length(E.lengths[b], E.most_len);
+    E.lengths_out[b] = length < E.budget ? length : E.budget;
+}
+
+template <bool kMove>
+void launch_select(const EvictParams &E, hipStream_t s) {
+    constexpr int kChunk = 256 * kSelectWaves;
+    const auto kernel = E.most_len <= kChunk       ? endor_kv_select_kernel<1, kMove>
+                        : E.most_len <= 2 * kChunk ? endor_kv_select_kernel<2, kMove>
+                        : E.most_len <= 4 * kChunk ? endor_kv_select_kernel<4, kMove>
+                        : E.most_len <= 8 * kChunk ? endor_kv_select_kernel<8, kMove>
+                                                   : endor_kv_select_kernel<0, kMove>;
+    hipLaunchKernelGGL(kernel, dim3(E.C.kv_heads, E.C.batch), dim3(kSelectThreads), 0, s, E);
+}
+
+// A workgroup moves so many tokens by itself sooner than a second launch begins.
+constexpr int kFewMoves = 64;
 
 // The most tokens of a sequence and head that move: as many as come free below the budget, or lie past it.
 int32_t most_moves(int32_t budget, int32_t len) {
@@ -235,10 +475,16 @@ extern "C" endor_status endor_kv_append(const endor_kv_cache *cache, const void 
     A.tokens = tokens;
     A.capacity = capacity_of(*cache);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (tokens > 0 && A.capacity > 0) {
-        hipLaunchKernelGGL(endor_kv_append_kernel, dim3(tokens, A.C.batch), dim3(256), 0, s, A);
-        if (hipGetLastError() != hipSuccess) return ENDOR_ERR_HIP;
+    const uint32_t units = A.C.dim / 8;
+    if (tokens <= static_cast<int>(kTokensEach)) {
+        const uint32_t rows = 2 * A.C.kv_heads * (tokens ? tokens : 1), most = 1024 / units;
+        hipLaunchKernelGGL(endor_kv_append_kernel, dim3(A.C.batch), dim3(units, rows < most ? rows : most), 0, s, A);
+        return hipGetLastError() == hipSuccess ? ENDOR_OK : ENDOR_ERR_HIP;
     }
+    const uint32_t lines = 256 / units, each = 4 * lines / (2 * kTokensEach) ? 4 * lines / (2 * kTokensEach) : 1, heads = A.C.kv_heads;
+    hipLaunchKernelGGL(endor_kv_append_many_kernel, dim3((static_cast<uint32_t>(tokens) + kTokensEach - 1) / kTokensEach, (heads + each - 1) / each, A.C.batch),
+                       dim3(units, lines), 0, s, A, each);
+    if (hipGetLastError() != hipSuccess) return ENDOR_ERR_HIP;
     hipLaunchKernelGGL(endor_kv_advance_kernel, dim3((A.C.batch + 255) / 256), dim3(256), 0, s, A);
     return hipGetLastError() == hipSuccess ? ENDOR_OK : ENDOR_ERR_HIP;
 }
@@ -282,9 +528,14 @@ extern "C" endor_status endor_kv_evict(const endor_kv_cache *cache, int32_t budg
     E.holes = E.count + rows;
     E.movers = E.holes + rows * E.most;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(endor_kv_select_kernel, dim3(E.C.kv_heads, E.C.batch), dim3(kSelectThreads), 0, s, E);
+    if (E.most <= kFewMoves) {
+        launch_select<true>(E, s);
+    } else {
+        launch_select<false>(E, s);
+        if (hipGetLastError() != hipSuccess) return ENDOR_ERR_HIP;
+        hipLaunchKernelGGL(endor_kv_move_kernel, dim3((E.most + kMovesEach - 1) / kMovesEach, E.C.kv_heads, E.C.batch), dim3(256), 0, s, E);
+    }
     if (hipGetLastError() != hipSuccess) return ENDOR_ERR_HIP;
-    const int64_t want = E.most < 1 ? 1 : E.most;
-    hipLaunchKernelGGL(endor_kv_move_kernel, dim3(static_cast<uint32_t>(want < 256 ? want : 256), E.C.kv_heads, E.C.batch), dim3(256), 0, s, E);
+    if (E.lengths_out == E.lengths) hipLaunchKernelGGL(endor_kv_shorten_kernel, dim3((E.C.batch + 255) / 256), dim3(256), 0, s, E);
     return hipGetLastError() == hipSuccess ? ENDOR_OK : ENDOR_ERR_HIP;
 }

@@ -19,52 +19,46 @@ class _Cache(ctypes.Structure):
                 ("head_dim", _i32), ("page_size", _i32), ("max_pages", _i32), ("dtype", _i32)]
 
 
-_declared = None
+_lib_declared = None
 
 
 def _lib():
-    global _declared
+    global _lib_declared
     L = binding.lib()
-    if _declared is not L:
-        L.endor_kv_append.argtypes = [_p, _p, _p, _i64, _i64, _i64, ctypes.c_int, _p, _p, _p, _p, _p, _p, _p, _p]
-        L.endor_attn_scratch_bytes.restype = _sz
-        L.endor_attn_scratch_bytes.argtypes = [_p, ctypes.c_int, _i32, ctypes.c_int]
-        L.endor_attn_decode.argtypes = [_p, ctypes.c_int, _p, _i64, _i64, _p, _i32, _p, _i64, ctypes.c_float, _p, _p, _p, _p, _p, _sz, _p]
-        L.endor_kv_evict_scratch_bytes.restype = _sz
-        L.endor_kv_evict_scratch_bytes.argtypes = [_p, _i32, _i32]
-        L.endor_kv_evict.argtypes = [_p, _i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p]
-        L.endor_q4_bytes.restype = _sz
-        L.endor_q4_bytes.argtypes = [_i64, _i64, ctypes.c_int, ctypes.c_int]
-        L.endor_q4_pack.argtypes = [_i64, _i64, ctypes.c_int, _p, _p, _p, _p, _sz, _p]
-        L.endor_q4_quantize.argtypes = [_i64, _i64, ctypes.c_int, _p, _p, _p, _p, _p]
-        L.endor_q4_scratch_bytes.restype = _sz
-        L.endor_q4_scratch_bytes.argtypes = [_i64, _i64, ctypes.c_int, ctypes.c_int]
-        L.endor_q4_gemm.argtypes = [_i64, _i64, ctypes.c_int, ctypes.c_int, _p, _sz, ctypes.c_int, _p, _i64, ctypes.c_int, _p, _p, _sz, _p]
-        _declared = L
+    if _lib_declared is not L:
+        for name, args in (
+                ("endor_kv_append", [_p, _p, _p, _i64, _i64, _i64, ctypes.c_int, _p, _p, _p, _p, _p, _p, _p, _p]),
+                ("endor_attn_decode", [_p, ctypes.c_int, _p, _i64, _i64, _p, _i32, _p, _i64, ctypes.c_float, _p, _p, _p, _p, _p, _sz, _p]),
+                ("endor_kv_evict", [_p, _i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p]),
+                ("endor_q4_pack", [_i64, _i64, ctypes.c_int, _p, _p, _p, _p, _sz, _p]),
+                ("endor_q4_quantize", [_i64, _i64, ctypes.c_int, _p, _p, _p, _p, _p]),
+                ("endor_q4_gemm", [_i64, _i64, ctypes.c_int, ctypes.c_int, _p, _sz, ctypes.c_int, _p, _i64, ctypes.c_int, _p, _p, _sz, _p])):
+            getattr(L, name).restype = ctypes.c_int
+            getattr(L, name).argtypes = args
+        for name, args in (("endor_attn_scratch_bytes", [_p, ctypes.c_int, _i32, ctypes.c_int]),
+                           ("endor_kv_evict_scratch_bytes", [_p, _i32, _i32]),
+                           ("endor_q4_bytes", [_i64, _i64, ctypes.c_int, ctypes.c_int]),
+                           ("endor_q4_scratch_bytes", [_i64, _i64, ctypes.c_int, ctypes.c_int])):
+            getattr(L, name).restype = _sz
+            getattr(L, name).argtypes = args
+        _lib_declared = L
     return L
+
+
+# The checks of a call are on the way of every token, and a tensor's attributes take 50 ns each: they are asked for
+# once, tensor by tensor, and not through helpers (an append took 10 us of the host with those, the kernel 4).
+
+def _bad(what):
+    raise ValueError(what)
 
 
 def _dtype_code(dtype):
     torch = _torch()
-    if dtype == torch.float16:
+    if dtype is torch.float16:
         return 0
-    if dtype == torch.bfloat16:
+    if dtype is torch.bfloat16:
         return 1
     raise ValueError("elements are float16 or bfloat16, got %s" % dtype)
-
-
-def _on(device, *tensors):
-    """All of the tensors that a kernel is to reach lie on that GPU."""
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError("all tensors must be on the cache's (the weight's) GPU")
-
-
-def _ints(t, count, name):
-    torch = _torch()
-    if t.dtype != torch.int32 or t.numel() != count or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous int32 tensor of %d elements" % (name, count))
-    return t
 
 
 class KVCache:
@@ -93,6 +87,7 @@ class KVCache:
         c.num_pages, c.pages_stride = self.num_pages, int(pages.stride(0)) if self.batch > 1 else self.max_pages
         c.batch, c.kv_heads, c.head_dim, c.page_size, c.max_pages = self.batch, self.kv_heads, self.head_dim, self.page_size, self.max_pages
         c.dtype = _dtype_code(k.dtype)
+        self.dtype = k.dtype
         self._at = ctypes.addressof(c)
 
     def _scratch(self, nbytes):
@@ -106,10 +101,24 @@ class KVCache:
         """Scratch of kv_evict, likewise."""
         return self._scratch(_lib().endor_kv_evict_scratch_bytes(self._at, budget, self.capacity if max_len is None else max_len))
 
-    def _per_slot(self, t, name, dtype):
-        if t.dtype != dtype or t.shape != (self.batch, self.kv_heads, self.capacity) or not t.is_contiguous():
-            raise ValueError("%s must be a contiguous %s tensor [batch, kv_heads, capacity]" % (name, dtype))
-        return t
+    def _per_sequence(self, *tensors):
+        i32, batch, device = _torch().int32, self.batch, self.device_index
+        for t in tensors:
+            if t.dtype is not i32 or t.get_device() != device or t.numel() != batch or not t.is_contiguous():
+                _bad("lengths, seen, counts and what they become must be contiguous int32 tensors [batch] on the cache's GPU")
+
+    def _per_slot(self, dtype, *tensors):
+        shape, device = (self.batch, self.kv_heads, self.capacity), self.device_index
+        for t in tensors:
+            if t is not None and (t.dtype is not dtype or t.get_device() != device or t.shape != shape or not t.is_contiguous()):
+                _bad("weights (float32) and positions (int32) must be contiguous tensors [batch, kv_heads, capacity] on the cache's GPU")
+
+    def _take(self, scratch):
+        if scratch is None:
+            return None, 0
+        if scratch.get_device() != self.device_index or not scratch.is_contiguous():
+            _bad("scratch must be contiguous, on the cache's GPU")
+        return scratch.data_ptr(), scratch.numel() * scratch.element_size()
 
 
 def kv_append(cache, k, v, lengths, seen=None, counts=None, weights=None, positions=None, new_lengths=None, new_seen=None, stream=None):
@@ -118,29 +127,35 @@ def kv_append(cache, k, v, lengths, seen=None, counts=None, weights=None, positi
     torch = _torch()
     if k.dim() == 3:
         k, v = k.unsqueeze(1), v.unsqueeze(1)
-    batch, tokens = cache.batch, int(k.shape[1])
-    if tuple(k.shape) != (batch, tokens, cache.kv_heads, cache.head_dim) or k.shape != v.shape or k.dtype != cache.k.dtype or v.dtype != k.dtype:
-        raise ValueError("k and v must be [batch, tokens, kv_heads, head_dim] of the cache's type")
-    if k.stride() != v.stride():
-        v = v.contiguous()
-        k = k.contiguous()
-    if k.stride(3) != 1 and cache.head_dim > 1:
-        raise ValueError("the last stride of k and v must be 1")
-    _ints(lengths, batch, "lengths")
-    seen = lengths if seen is None else _ints(seen, batch, "seen")
-    if counts is not None:
-        _ints(counts, batch, "counts")
-    if weights is not None:
-        cache._per_slot(weights, "weights", torch.float32)
-    if positions is not None:
-        cache._per_slot(positions, "positions", torch.int32)
-    new_lengths = torch.empty_like(lengths) if new_lengths is None else _ints(new_lengths, batch, "new_lengths")
-    new_seen = torch.empty_like(seen) if new_seen is None else _ints(new_seen, batch, "new_seen")
-    _on(cache.device_index, k, v, lengths, seen, counts, weights, positions, new_lengths, new_seen)
+    shape, dtype, device = k.shape, cache.dtype, cache.device_index
+    if len(shape) != 4 or v.shape != shape or k.dtype is not dtype or v.dtype is not dtype or k.get_device() != device or v.get_device() != device:
+        _bad("k and v must be [batch, tokens, kv_heads, head_dim] of the cache's type, on its GPU")
+    batch, tokens, heads, dim = shape
+    if batch != cache.batch or heads != cache.kv_heads or dim != cache.head_dim:
+        _bad("k and v must be [batch, tokens, kv_heads, head_dim] of the cache")
     st = k.stride()
-    _check(_lib().endor_kv_append(cache._at, _dptr(k), _dptr(v), st[0], st[1], st[2], tokens, _dptr(counts), _dptr(lengths), _dptr(seen),
-                                  _dptr(new_lengths), _dptr(new_seen), _dptr(weights), _dptr(positions), _stream_handle(stream)),
-           "endor_kv_append")
+    if v.stride() != st or st[3] != 1:
+        k, v = k.contiguous(), v.contiguous()
+        st = k.stride()
+    if seen is None:
+        seen = lengths
+    if new_lengths is None:
+        new_lengths = torch.empty_like(lengths)
+    if new_seen is None:
+        new_seen = torch.empty_like(seen)
+    cache._per_sequence(lengths, seen, new_lengths, new_seen)
+    if counts is not None:
+        cache._per_sequence(counts)
+    if weights is not None:
+        cache._per_slot(torch.float32, weights)
+    if positions is not None:
+        cache._per_slot(torch.int32, positions)
+    status = _lib().endor_kv_append(cache._at, k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], tokens, None if counts is None else counts.data_ptr(),
+                                    lengths.data_ptr(), seen.data_ptr(), new_lengths.data_ptr(), new_seen.data_ptr(),
+                                    None if weights is None else weights.data_ptr(), None if positions is None else positions.data_ptr(),
+                                    _stream_handle(stream))
+    if status:
+        _check(status, "endor_kv_append")
     return new_lengths, new_seen
 
 
@@ -151,38 +166,43 @@ def attn_decode(cache, q, lengths, max_len=None, mask=None, scale=None, weights=
     to head_dim ** -0.5.  With new_weights the tokens' attention weights are added to `weights` (None: to 0) into it.
     Returns (out, lse)."""
     torch = _torch()
-    batch, max_len = cache.batch, cache.capacity if max_len is None else int(max_len)
-    if q.dim() != 3 or q.shape[0] != batch or q.shape[2] != cache.head_dim or q.dtype != cache.k.dtype or (cache.head_dim > 1 and q.stride(2) != 1):
-        raise ValueError("q must be [batch, q_heads, head_dim] of the cache's type, its last stride 1")
-    q_heads = int(q.shape[1])
-    _ints(lengths, batch, "lengths")
-    mask_stride = 0
+    batch, device = cache.batch, cache.device_index
+    max_len = cache.capacity if max_len is None else max_len
+    shape = q.shape
+    if len(shape) != 3 or q.dtype is not cache.dtype or q.get_device() != device or shape[0] != batch or shape[2] != cache.head_dim:
+        _bad("q must be [batch, q_heads, head_dim] of the cache's type, on its GPU")
+    q_heads, st = shape[1], q.stride()
+    if st[2] != 1:
+        _bad("the last stride of q must be 1")
+    cache._per_sequence(lengths)
+    mask_at, mask_stride = None, 0
     if mask is not None:
         words = (min(max_len, cache.capacity) + 63) // 64
-        if mask.dtype != torch.int64 or mask.dim() != 2 or mask.shape[0] != batch or mask.shape[1] < words or (mask.shape[1] > 1 and mask.stride(1) != 1):
-            raise ValueError("mask must be an int64 tensor [batch, >= %d] with contiguous rows" % words)
-        mask_stride = int(mask.stride(0))
-    if weights is not None:
-        cache._per_slot(weights, "weights", torch.float32)
-        if new_weights is None:
-            raise ValueError("weights without new_weights: pass the buffer for the sums, which may be weights itself")
+        if (mask.dtype is not torch.int64 or mask.dim() != 2 or mask.shape[0] != batch or mask.shape[1] < words or mask.get_device() != device
+                or (mask.shape[1] > 1 and mask.stride(1) != 1)):
+            _bad("mask must be an int64 tensor [batch, >= %d] with contiguous rows, on the cache's GPU" % words)
+        mask_at, mask_stride = mask.data_ptr(), mask.stride(0) if batch > 1 else mask.shape[1]
+    if weights is not None and new_weights is None:
+        _bad("weights without new_weights: pass the buffer for the sums, which may be weights itself")
     if new_weights is not None:
-        cache._per_slot(new_weights, "new_weights", torch.float32)
+        cache._per_slot(torch.float32, weights, new_weights)
     if out is None:
         out = torch.empty((batch, q_heads, cache.head_dim), dtype=q.dtype, device=q.device)
-    elif out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous():
-        raise ValueError("out must be a contiguous tensor like q")
+    elif out.dtype is not cache.dtype or out.shape != shape or out.get_device() != device or not out.is_contiguous():
+        _bad("out must be a contiguous tensor like q")
     if lse is None:
         lse = torch.empty((batch, q_heads), dtype=torch.float32, device=q.device)
-    elif lse.dtype != torch.float32 or lse.numel() != batch * q_heads or not lse.is_contiguous():
-        raise ValueError("lse must be a contiguous float32 tensor [batch, q_heads]")
+    elif lse.dtype is not torch.float32 or lse.numel() != batch * q_heads or lse.get_device() != device or not lse.is_contiguous():
+        _bad("lse must be a contiguous float32 tensor [batch, q_heads]")
     if scratch is None:
         scratch = cache.attn_scratch(q_heads, max_len, new_weights is not None)
-    _on(cache.device_index, q, lengths, mask, weights, new_weights, out, lse, scratch)
-    _check(_lib().endor_attn_decode(cache._at, q_heads, _dptr(q), q.stride(0), q.stride(1), _dptr(lengths), max_len, _dptr(mask), mask_stride,
-                                    cache.head_dim ** -0.5 if scale is None else scale, _dptr(out), _dptr(lse), _dptr(weights),
-                                    _dptr(new_weights), _dptr(scratch), 0 if scratch is None else scratch.numel(), _stream_handle(stream)),
-           "endor_attn_decode")
+    scratch_at, room = cache._take(scratch)
+    status = _lib().endor_attn_decode(cache._at, q_heads, q.data_ptr(), st[0], st[1], lengths.data_ptr(), max_len, mask_at, mask_stride,
+                                      cache.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr(),
+                                      None if weights is None else weights.data_ptr(), None if new_weights is None else new_weights.data_ptr(),
+                                      scratch_at, room, _stream_handle(stream))
+    if status:
+        _check(status, "endor_attn_decode")
     return out, lse
 
 
@@ -191,20 +211,21 @@ def kv_evict(cache, lengths, seen, weights, positions, budget, recent, max_len=N
     """endor_kv_evict: every kv head of every sequence keeps `budget` tokens, the newest `recent` and those of the largest weight.
     Returns (new_lengths, new_weights, new_positions); pass the inputs for them to change in place."""
     torch = _torch()
-    max_len = cache.capacity if max_len is None else int(max_len)
-    _ints(lengths, cache.batch, "lengths")
-    _ints(seen, cache.batch, "seen")
-    cache._per_slot(weights, "weights", torch.float32)
-    cache._per_slot(positions, "positions", torch.int32)
-    new_lengths = torch.empty_like(lengths) if new_lengths is None else _ints(new_lengths, cache.batch, "new_lengths")
-    new_weights = torch.zeros_like(weights) if new_weights is None else cache._per_slot(new_weights, "new_weights", torch.float32)
-    new_positions = torch.zeros_like(positions) if new_positions is None else cache._per_slot(new_positions, "new_positions", torch.int32)
+    max_len = cache.capacity if max_len is None else max_len
+    new_lengths = torch.empty_like(lengths) if new_lengths is None else new_lengths
+    new_weights = torch.zeros_like(weights) if new_weights is None else new_weights
+    new_positions = torch.zeros_like(positions) if new_positions is None else new_positions
+    cache._per_sequence(lengths, seen, new_lengths)
+    cache._per_slot(torch.float32, weights, new_weights)
+    cache._per_slot(torch.int32, positions, new_positions)
     if scratch is None:
         scratch = cache.evict_scratch(budget, max_len)
-    _on(cache.device_index, lengths, seen, weights, positions, new_lengths, new_weights, new_positions, scratch)
-    _check(_lib().endor_kv_evict(cache._at, budget, recent, max_len, _dptr(lengths), _dptr(seen), _dptr(weights), _dptr(positions),
-                                 _dptr(new_lengths), _dptr(new_weights), _dptr(new_positions), _dptr(scratch),
-                                 0 if scratch is None else scratch.numel(), _stream_handle(stream)), "endor_kv_evict")
+    scratch_at, room = cache._take(scratch)
+    status = _lib().endor_kv_evict(cache._at, budget, recent, max_len, lengths.data_ptr(), seen.data_ptr(), weights.data_ptr(), positions.data_ptr(),
+                                   new_lengths.data_ptr(), new_weights.data_ptr(), new_positions.data_ptr(), scratch_at, room,
+                                   _stream_handle(stream))
+    if status:
+        _check(status, "endor_kv_evict")
     return new_lengths, new_weights, new_positions
 
 
@@ -240,7 +261,8 @@ def q4_pack(codes, scales, zeros, cols, group, stream=None):
         raise ValueError("zeros must be a contiguous uint8 tensor [rows, ceil(cols / group)]")
     if not codes.is_cuda:
         raise ValueError("codes must lie in GPU memory")
-    _on(codes.get_device(), scales, zeros)
+    if any(t is not None and t.get_device() != codes.get_device() for t in (scales, zeros)):
+        raise ValueError("codes, scales and zeros must be on one GPU")
     L = _lib()
     packed = torch.empty(L.endor_q4_bytes(rows, cols, group, int(zeros is not None)), dtype=torch.uint8, device=codes.device)
     _check(L.endor_q4_pack(rows, cols, group, _dptr(codes), _dptr(scales), _dptr(zeros), _dptr(packed), packed.numel(), _stream_handle(stream)),
@@ -274,20 +296,28 @@ def q4_scratch_bytes(m, nb):
 def q4_gemm(m, X, Y=None, scratch=None, stream=None):
     """endor_q4_gemm: Y (fp32, nb x rows) = X W^T; X: (nb, cols) float16 or bfloat16 (row stride = ldx), nb <= 16."""
     torch = _torch()
-    if X.dim() != 2 or X.shape[1] != m.cols or (m.cols > 1 and X.stride(1) != 1):
-        raise ValueError("X must be (nb, cols) with contiguous rows")
-    nb = int(X.shape[0])
+    shape, rows, device = X.shape, m.rows, m.packed.get_device()
+    if len(shape) != 2 or shape[1] != m.cols or X.get_device() != device:
+        _bad("X must be (nb, cols), on the weight's GPU")
+    nb, (ldx, inner) = shape[0], X.stride()
+    if inner != 1 and m.cols > 1:
+        _bad("X must have contiguous rows")
     if Y is None:
-        Y = torch.empty((nb, m.rows), dtype=torch.float32, device=X.device)
-    elif Y.dtype != torch.float32 or Y.numel() != nb * m.rows or not Y.is_contiguous():
-        raise ValueError("Y must be a contiguous fp32 tensor of nb*rows elements")
+        Y = torch.empty((nb, rows), dtype=torch.float32, device=X.device)
+    elif Y.dtype is not torch.float32 or Y.numel() != nb * rows or Y.get_device() != device or not Y.is_contiguous():
+        _bad("Y must be a contiguous fp32 tensor of nb*rows elements, on the weight's GPU")
     L = _lib()
+    scratch_at, room = None, 0
     if scratch is None:
-        need = L.endor_q4_scratch_bytes(m.rows, m.cols, m.group, nb)
-        if need:
-            scratch = torch.empty(need, dtype=torch.uint8, device=X.device)
-    _on(m.packed.get_device(), X, Y, scratch)
-    ldx = X.stride(0) if nb > 1 else m.cols
-    _check(L.endor_q4_gemm(m.rows, m.cols, m.group, m.zeros, _dptr(m.packed), m.packed.numel(), _dtype_code(X.dtype), _dptr(X), ldx, nb,
-                           _dptr(Y), _dptr(scratch), 0 if scratch is None else scratch.numel(), _stream_handle(stream)), "endor_q4_gemm")
+        room = L.endor_q4_scratch_bytes(rows, m.cols, m.group, nb)
+        if room:
+            scratch = torch.empty(room, dtype=torch.uint8, device=X.device)
+    elif scratch.get_device() != device or not scratch.is_contiguous():
+        _bad("scratch must be contiguous, on the weight's GPU")
+    if scratch is not None:
+        scratch_at, room = scratch.data_ptr(), scratch.numel() * scratch.element_size()
+    status = L.endor_q4_gemm(rows, m.cols, m.group, m.zeros, m.packed.data_ptr(), m.packed.numel(), _dtype_code(X.dtype), X.data_ptr(),
+                             ldx if nb > 1 else m.cols, nb, Y.data_ptr(), scratch_at, room, _stream_handle(stream))
+    if status:
+        _check(status, "endor_q4_gemm")
     return Y
