@@ -328,43 +328,71 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : kDim == 128 ? 2 : 4)
 // Maximum and total of a query head over its sequence's splits; every lane of the wave gets them.
 __device__ __forceinline__ float2 joined(const float2 *ml, int32_t splits, uint32_t lane) {
     float m = -INFINITY, all = 0;
-    for (int32_t s = lane; s < splits; s += 64) m = fmaxf(m, ml[s].x);
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    for (int32_t s = lane; s < splits; s += 64) all += ml[s].x == -INFINITY ? 0.0f : ml[s].y * __builtin_amdgcn_exp2f(ml[s].x - m);
+    for (int32_t s0 = 0; s0 < splits; s0 += 256) {  // four splits of every lane on their way
+        float2 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t s = s0 + 64 * i + static_cast<int32_t>(lane);
+            x[i] = ml[s < splits ? s : splits - 1];
+            if (s >= splits) x[i] = make_float2(-INFINITY, 0.0f);
+        }
+        float most = m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = fmaxf(most, x[i].x);
+        all = m == -INFINITY ? 0.0f : all * __builtin_amdgcn_exp2f(m - most);
+        m = most;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) all += x[i].x == -INFINITY ? 0.0f : x[i].y * __builtin_amdgcn_exp2f(x[i].x - m);
+    }
+    float most = m;
+    for (int d = 32; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    all = m == -INFINITY ? 0.0f : all * __builtin_amdgcn_exp2f(m - most);
     for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d);
-    return make_float2(m, all);
+    return make_float2(most, all);
 }
 
-constexpr int kSlots = 1024;  // slots of a workgroup that adds weights
+constexpr int kJoinThreads = 512;
+constexpr int kSlots = 2048;  // slots of a workgroup that adds weights
 
-// Workgroups below batch * q_heads join a head's splits (if there are several), the others add the weights of kSlots slots of a kv head.
+// Workgroups below batch * q_heads join a head's splits (if there are several): a thread takes four dims of every so many splits.  The others add the
+// weights of kSlots slots of a kv head.
 template <bool kBf16>
-__global__ __launch_bounds__(256) void endor_attn_join_kernel(AttnParams A, uint32_t joins, uint32_t pieces) {
-    __shared__ float s_sum[4][256];
+__global__ __launch_bounds__(kJoinThreads) void endor_attn_join_kernel(AttnParams A, uint32_t joins, uint32_t pieces) {
+    __shared__ f32x4 s_sum[kJoinThreads];
+    __shared__ float s_off[256];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (blockIdx.x < joins) {
         const int64_t row = blockIdx.x, b = row / A.q_heads;
         const int32_t length = clamp_length(A.lengths[b], A.most_len), dim = A.C.dim;
         const int32_t splits = length > 0 ? (length + A.chunk - 1) / A.chunk : 1;
         const float2 *ml = A.ml + row * A.splits;
+        const int32_t units = dim / 4, lines = kJoinThreads / units, line = threadIdx.x / units, d = 4 * (threadIdx.x % units);
+        const float *from = A.partial + row * A.splits * dim + d;
         const float2 all = joined(ml, splits, lane);
-        float sum[4] = {0, 0, 0, 0};
-        for (int32_t s = wave; s < splits; s += 4) {
-            const float share = ml[s].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[s].x - all.x);
-            const float *from = A.partial + (row * A.splits + s) * dim;
+        f32x4 sum = {0, 0, 0, 0};
+        if (line < lines)
+            for (int32_t s0 = line; s0 < splits; s0 += 4 * lines) {
+                f32x4 x[4];
+                float share[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (static_cast<int32_t>(64 * i + lane) < dim) sum[i] += share * from[64 * i + lane];
-        }
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t s = s0 + i * lines < splits ? s0 + i * lines : s0;
+                    x[i] = *reinterpret_cast<const f32x4 *>(from + int64_t(s) * dim);
+                    share[i] = ml[s].x;
+                }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s_sum[wave][64 * i + lane] = sum[i];
+                for (int i = 0; i < 4; ++i)
+                    if (s0 + i * lines < splits && share[i] != -INFINITY) sum += __builtin_amdgcn_exp2f(share[i] - all.x) * x[i];
+            }
+        s_sum[threadIdx.x] = sum;
         __syncthreads();
-        const int32_t d = threadIdx.x;
-        if (d < dim) {
-            const float x = s_sum[0][d] + s_sum[1][d] + s_sum[2][d] + s_sum[3][d];
-            A.out[row * dim + d] = narrow<kBf16>(all.y == 0 ? 0.0f : x / all.y);
+        if (static_cast<int32_t>(threadIdx.x) < dim) {
+            const float *part = reinterpret_cast<const float *>(s_sum) + threadIdx.x;
+            float x = 0;
+            for (int32_t l = 0; l < lines && l < splits; ++l) x += part[l * dim];
+            A.out[row * dim + threadIdx.x] = narrow<kBf16>(all.y == 0 ? 0.0f : x / all.y);
         }
-        if (d == 0 && A.lse) A.lse[row] = all.y == 0 ? -INFINITY : (all.x - kShift + log2f(all.y)) * kLn2;
+        if (threadIdx.x == 0 && A.lse) A.lse[row] = all.y == 0 ? -INFINITY : (all.x - kShift + log2f(all.y)) * kLn2;
         return;
     }
     const uint32_t unit = (blockIdx.x - joins) / pieces, piece = (blockIdx.x - joins) % pieces;
@@ -374,31 +402,40 @@ __global__ __launch_bounds__(256) void endor_attn_join_kernel(AttnParams A, uint
     if (t0 >= length) return;
     const int32_t splits = (length + A.chunk - 1) / A.chunk;
     const int64_t row0 = int64_t(b) * A.q_heads + int64_t(kv) * A.group;
-    float sum[kSlots / 256] = {};
+    // four slots to a thread; rows of logits are whole tiles, so that a unit that begins below the length can be read
+    const int32_t t = t0 + 4 * static_cast<int32_t>(threadIdx.x);
+    const bool in = t < length;
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    const int64_t at = (int64_t(b) * A.C.kv_heads + kv) * A.capacity + t;
+    f32x4 sum = {0, 0, 0, 0};
+    if (in && A.weights) sum = *reinterpret_cast<const f32x4_any *>(A.weights + at);  // the capacity is whole pages, of 8 slots at least
+    f32x4 added = {0, 0, 0, 0};
     for (int32_t h0 = 0; h0 < A.group && A.C.num_pages; h0 += 256) {
         const int32_t heads = A.group - h0 < 256 ? A.group - h0 : 256;
         __syncthreads();
-        for (int32_t h = wave; h < heads; h += 4) {
+        for (int32_t h = wave; h < heads; h += kJoinThreads / 64) {
             const float2 all = joined(A.ml + (row0 + h0 + h) * A.splits, splits, lane);
             // what is taken off a logit: all of them are -infinity where nothing is visible
-            if (lane == 0) s_sum[0][h] = all.y == 0 ? 0.0f : all.x - kShift + log2f(all.y);
+            if (lane == 0) s_off[h] = all.y == 0 ? 0.0f : all.x - kShift + log2f(all.y);
         }
         __syncthreads();
-        for (int32_t h = 0; h < heads; ++h) {
-            const float off = s_sum[0][h];
-            const float *logit = A.logits + (row0 + h0 + h) * A.row;
+        if (in) {
+            const float *logit = A.logits + (row0 + h0) * A.row + t;
+#pragma unroll 4
+            for (int32_t h = 0; h < heads; ++h) {
+                const f32x4 s = *reinterpret_cast<const f32x4 *>(logit + int64_t(h) * A.row);
 #pragma unroll
-            for (int i = 0; i < kSlots / 256; ++i) {
-                const int32_t t = t0 + 256 * i + threadIdx.x;
-                if (t < length) sum[i] += __builtin_amdgcn_exp2f(logit[t] - off);
+                for (int i = 0; i < 4; ++i) added[i] += __builtin_amdgcn_exp2f(s[i] - s_off[h]);
             }
         }
     }
-    const int64_t base = (int64_t(b) * A.C.kv_heads + kv) * A.capacity;
+    sum += added;
+    if (t + 4 <= length) {
+        *reinterpret_cast<f32x4_any *>(A.weights_out + at) = sum;
+    } else if (in) {
 #pragma unroll
-    for (int i = 0; i < kSlots / 256; ++i) {
-        const int32_t t = t0 + 256 * i + threadIdx.x;
-        if (t < length) A.weights_out[base + t] = (A.weights ? A.weights[base + t] : 0.0f) + sum[i];
+        for (int i = 0; i < 4; ++i)
+            if (t + i < length) A.weights_out[at + i] = sum[i];
     }
 }
 
@@ -475,7 +512,7 @@ extern "C" endor_status endor_attn_decode(const endor_kv_cache *cache, int q_hea
     const uint32_t pieces = d_weights_out ? (A.most_len + kSlots - 1) / kSlots : 0;
     const uint32_t groups = joins + pieces * static_cast<uint32_t>(A.C.batch) * A.C.kv_heads;
     if (groups) {
-        hipLaunchKernelGGL(bf16 ? endor_attn_join_kernel<true> : endor_attn_join_kernel<false>, dim3(groups), dim3(256), 0, s, A, joins, pieces);
+        hipLaunchKernelGGL(bf16 ? endor_attn_join_kernel<true> : endor_attn_join_kernel<false>, dim3(groups), dim3(kJoinThreads), 0, s, A, joins, pieces);
         if (hipGetLastError() != hipSuccess) return ENDOR_ERR_HIP;
     }
     return ENDOR_OK;

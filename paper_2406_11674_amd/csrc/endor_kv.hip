@@ -143,10 +143,16 @@ constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kBinBits = 11, kBins = 1 << kBinBits;  // of a pass over the keys
 static_assert(kBins == 2 * kSelectThreads, "a thread reads two bins");
 
+// A workgroup moves so many tokens by itself sooner than a second launch begins.
+constexpr int kFewMoves = 64;
+
 struct SelectShared {
     uint32_t bins[kBins];
     uint32_t part[2][kSelectWaves];
+    uint32_t low[kSelectWaves], high[kSelectWaves];
     uint32_t found[3];  // the bin that the last kept key is in, the keys above it, the keys in it
+    uint32_t left, last[64];  // the keys in question, when a wave can hold them
+    int32_t holes[kFewMoves], movers[kFewMoves];
 };
 
 // Exclusive prefix over the workgroup, and the total.  `turn` changes from one call to the next, so that one barrier does.
@@ -197,8 +203,8 @@ __device__ __forceinline__ void move_units(const Cache &C, const int32_t *table,
 // kept ones past it, in order.
 //
 // The keys are looked at 11 bits at a time from the highest bit in which they differ: a histogram in LDS, and a scan of it from
-// the top, three passes at most.  (Weights of one row share most of their leading bits: a fixed first digit would have nearly
-// all keys in a few bins, where LDS adds them one after the other.)  A wave has a contiguous piece of the slots, 256 of them at a
+// the top, until a wave can hold what is left and count for each key those above it.  (Weights of one row share most of their leading
+// bits: a fixed first digit would have nearly all keys in a few bins, where LDS adds them one after the other.)  A wave has a contiguous piece of the slots, 256 of them at a
 // time, four to a lane: loads are whole lines, and ranks in the order of slots need wave scans only.  kChunks: such chunks of a wave that it
 // keeps as keys in registers; 0: the keys are formed anew in every pass, for rows past 32768 slots.
 // kMove: the moves are few and done here.
@@ -246,10 +252,26 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         }
         return key;
     };
+    S.bins[threadIdx.x] = 0;
+    S.bins[threadIdx.x + kSelectThreads] = 0;
+    if (threadIdx.x == 0) S.left = 0;
     u32x4 held[kChunks ? kChunks : 1];
     if constexpr (kChunks > 0)
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) held[i] = keys_at(mine + 256 * i);
+    // Slots below the budget as they are; those that come free are written again behind several barriers.
+    if (copies)
+        for (uint32_t t = mine, i = 0; i < chunks; ++i, t += 256) {
+            if (t + 4 <= budget) {  // which is below the length
+                *reinterpret_cast<f32x4_any *>(w_out + t) = *reinterpret_cast<const f32x4_any *>(w + t);
+                *reinterpret_cast<i32x4_any *>(pos_out + t) = *reinterpret_cast<const i32x4_any *>(pos + t);
+            } else {
+                for (uint32_t e = 0; e < 4 && t + e < budget; ++e) {
+                    w_out[t + e] = w[t + e];
+                    pos_out[t + e] = pos[t + e];
+                }
+            }
+        }
     // f(slot of four keys, the keys) for all of the lane's
     auto each = [&](auto f) {
         if constexpr (kChunks > 0) {
@@ -281,15 +303,15 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         high = u > high ? u : high;
     }
     if (lane == 0) {
-        S.bins[2 * wave] = low;
-        S.bins[2 * wave + 1] = high;
+        S.low[wave] = low;
+        S.high[wave] = high;
     }
     group_scan(staying, S, turn++, &total);  // its barrier is for both
     staying = total;
 #pragma unroll
     for (int v = 0; v < kSelectWaves; ++v) {
-        low = S.bins[2 * v] < low ? S.bins[2 * v] : low;
-        high = S.bins[2 * v + 1] > high ? S.bins[2 * v + 1] : high;
+        low = S.low[v] < low ? S.low[v] : low;
+        high = S.high[v] > high ? S.high[v] : high;
     }
     uint32_t least = kStay, ties = budget;  // keys above `least` stay, and the first `ties` of those equal to it
     if (staying < budget) {
@@ -299,17 +321,16 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         uint32_t shift = range >> kBinBits ? 32 - __clz(range) - kBinBits : 0;
         uint64_t width = uint64_t(range) + 1;  // keys in [low, low + width) are still in question
         for (;;) {
-            __syncthreads();  // the bins are not read any more
-            S.bins[threadIdx.x] = 0;
-            S.bins[threadIdx.x + kSelectThreads] = 0;
-            __syncthreads();
+            auto in_question = [&](uint32_t t, uint32_t key) { return t < length && key != kStay && key >= low && key - low < width; };
             each([&](uint32_t t, u32x4 key) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (t + e < length && key[e] != kStay && key[e] >= low && key[e] - low < width) atomicAdd(&S.bins[(key[e] - low) >> shift], 1u);
+                    if (in_question(t + e, key[e])) atomicAdd(&S.bins[(key[e] - low) >> shift], 1u);
             });
             __syncthreads();
             const uint32_t top = kBins - 1 - 2 * threadIdx.x, c0 = S.bins[top], c1 = S.bins[top - 1];
+            S.bins[top] = 0;
+            S.bins[top - 1] = 0;
             const uint32_t above = group_scan(c0 + c1, S, turn++, &total);
             if (above < need && above + c0 + c1 >= need) {
                 const bool second = above + c0 < need;
@@ -318,15 +339,37 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
                 S.found[2] = second ? c1 : c0;
             }
             __syncthreads();
+            const uint32_t in_bin = S.found[2];
             low += S.found[0] << shift;
             need -= S.found[1];
-            if (shift == 0 || need == S.found[2]) {
+            if (shift == 0 || need == in_bin) {
                 least = low;
                 ties = shift == 0 ? need : 0xffffffffu;  // all of the bin stay: those from its lower end on
                 break;
             }
             width = uint64_t(1) << shift;
             shift = shift > kBinBits ? shift - kBinBits : 0;
+            if (in_bin <= 64) {
+                each([&](uint32_t t, u32x4 key) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (in_question(t + e, key[e])) S.last[atomicAdd(&S.left, 1u)] = key[e];
+                });
+                __syncthreads();
+                const uint32_t key = lane < in_bin ? S.last[lane] : 0;
+                uint32_t over = 0, same = 0;
+                for (uint32_t i = 0; i < in_bin; ++i) {
+                    const uint32_t other = __builtin_amdgcn_readlane(key, i);
+                    over += other > key;
+                    same += other == key;
+                }
+                // the lanes that hold the last key to stay; all waves find the same
+                const uint64_t at = __ballot(lane < in_bin && over < need && over + same >= need);
+                const uint32_t from = __builtin_ctzll(at);
+                least = __builtin_amdgcn_readlane(key, from);
+                ties = need - __builtin_amdgcn_readlane(over, from);
+                break;
+            }
         }
     }
 
@@ -374,7 +417,7 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         movers_mine += __popc(kept & ~below(t, budget));
     });
     uint32_t holes = waves_before(holes_mine), movers = waves_before(movers_mine);
-    int32_t *hole_list = E.holes + row * E.most, *mover_list = E.movers + row * E.most;
+    int32_t *hole_list = kMove ? S.holes : E.holes + row * E.most, *mover_list = kMove ? S.movers : E.movers + row * E.most;
     each_kept([&](uint32_t t, uint32_t kept) {
         const uint32_t free = below(t, budget) & ~kept, past = kept & ~below(t, budget);
         const uint32_t f = wave_inclusive_scan(__popc(free)), m = wave_inclusive_scan(__popc(past));
@@ -383,10 +426,6 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         for (int e = 0; e < 4; ++e) {
             if (free >> e & 1) hole_list[at++] = t + e;
             if (past >> e & 1) mover_list[to++] = t + e;
-            if (copies && (kept & below(t, budget)) >> e & 1) {
-                w_out[t + e] = w[t + e];
-                pos_out[t + e] = pos[t + e];
-            }
         }
         holes += __builtin_amdgcn_readlane(f, 63);
         movers += __builtin_amdgcn_readlane(m, 63);
@@ -436,9 +475,6 @@ void launch_select(const EvictParams &E, hipStream_t s) {
                                                    : endor_kv_select_kernel<0, kMove>;
     hipLaunchKernelGGL(kernel, dim3(E.C.kv_heads, E.C.batch), dim3(kSelectThreads), 0, s, E);
 }
-
-// A workgroup moves so many tokens by itself sooner than a second launch begins.
-constexpr int kFewMoves = 64;
 
 // The most tokens of a sequence and head that move: as many as come free below the budget, or lie past it.
 int32_t most_moves(int32_t budget, int32_t len) {
