@@ -143,6 +143,16 @@ constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kBinBits = 11, kBins = 1 << kBinBits;  // of a pass over the keys
 static_assert(kBins == 2 * kSelectThreads, "a thread reads two bins");
 
+// Where a token's keys and values are and go: element offsets from the pools' beginnings; -1 where a page is not there.
+struct Move {
+    int64_t from, to;
+};
+__device__ __forceinline__ Move move_of(const Cache &C, const int32_t *table, uint32_t h, uint32_t to, uint32_t from) {
+    uint32_t a, z;
+    const bool here = page_of(C, table, to, &a), there = page_of(C, table, from, &z);
+    return here && there ? Move{slot_at(C, z, h, from), slot_at(C, a, h, to)} : Move{-1, -1};
+}
+
 // A workgroup moves so many tokens by itself sooner than a second launch begins.
 constexpr int kFewMoves = 64;
 
@@ -151,8 +161,9 @@ struct SelectShared {
     uint32_t part[2][kSelectWaves];
     uint32_t low[kSelectWaves], high[kSelectWaves];
     uint32_t found[3];  // the bin that the last kept key is in, the keys above it, the keys in it
-    uint32_t left, last[64];  // the keys in question, when a wave can hold them
+    uint32_t left, last[64], over[64], same[64];  // the keys in question, when a wave can hold them; the keys above each and its equals
     int32_t holes[kFewMoves], movers[kFewMoves];
+    Move moves[kFewMoves];
 };
 
 // Exclusive prefix over the workgroup, and the total.  `turn` changes from one call to the next, so that one barrier does.
@@ -171,31 +182,24 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t x, SelectShared &S, uint
     return before + upto - x;
 }
 
-// A token's keys and values from one slot to another: 16 bytes a lane, K and V side by side.  `per`: units of a token.
-__device__ __forceinline__ void move_units(const Cache &C, const int32_t *table, uint32_t h, const int32_t *to, const int32_t *from, uint32_t first,
-                                           uint32_t count, uint32_t thread, uint32_t threads) {
-    const uint32_t half = C.dim / 8, per = 2 * half;
-    for (uint32_t u0 = thread; u0 < count * per; u0 += 4 * threads) {
+// Moves tokens, 16 bytes a lane, keys and values side by side, four loads of a thread on their way.
+__device__ __forceinline__ void move_tokens(const Cache &C, const Move *moves, uint32_t count, uint32_t threads) {
+    const uint32_t half = C.dim / 8, per = 2 * half, lines = threads / per, line = threadIdx.x / per, part = threadIdx.x % per;
+    uint16_t *pool = (part < half ? C.k : C.v) + 8 * (part < half ? part : part - half);
+    if (line >= lines) return;
+    for (uint32_t i0 = line; i0 < count; i0 += 4 * lines) {
         u32x4 held[4];
-        uint16_t *dst[4];
+        int64_t to[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t u = u0 + k * threads;
-            dst[k] = nullptr;
-            if (u < count * per) {
-                const uint32_t i = first + u / per, part = u % per, a = to[i], z = from[i];
-                uint32_t a_page, z_page;
-                if (page_of(C, table, a, &a_page) && page_of(C, table, z, &z_page)) {
-                    uint16_t *pool = part < half ? C.k : C.v;
-                    const uint32_t d = 8 * (part < half ? part : part - half);
-                    held[k] = *reinterpret_cast<const u32x4 *>(pool + slot_at(C, z_page, h, z) + d);
-                    dst[k] = pool + slot_at(C, a_page, h, a) + d;
-                }
-            }
+            const uint32_t i = i0 + k * lines;
+            const Move m = moves[i < count ? i : i0];
+            to[k] = i < count ? m.to : -1;
+            held[k] = *reinterpret_cast<const u32x4 *>(pool + (m.from < 0 ? 0 : m.from));  // the pool has a first page: something is to be moved
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if (dst[k]) *reinterpret_cast<u32x4 *>(dst[k]) = held[k];
+            if (to[k] >= 0) *reinterpret_cast<u32x4 *>(pool + to[k]) = held[k];
     }
 }
 
@@ -254,6 +258,7 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
     };
     S.bins[threadIdx.x] = 0;
     S.bins[threadIdx.x + kSelectThreads] = 0;
+    if (threadIdx.x < 64) S.over[threadIdx.x] = S.same[threadIdx.x] = 0;
     if (threadIdx.x == 0) S.left = 0;
     u32x4 held[kChunks ? kChunks : 1];
     if constexpr (kChunks > 0)
@@ -358,11 +363,16 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
                 __syncthreads();
                 const uint32_t key = lane < in_bin ? S.last[lane] : 0;
                 uint32_t over = 0, same = 0;
-                for (uint32_t i = 0; i < in_bin; ++i) {
-                    const uint32_t other = __builtin_amdgcn_readlane(key, i);
+                for (uint32_t i = wave; i < in_bin; i += kSelectWaves) {
+                    const uint32_t other = S.last[i];
                     over += other > key;
                     same += other == key;
                 }
+                atomicAdd(&S.over[lane], over);
+                atomicAdd(&S.same[lane], same);
+                __syncthreads();
+                over = S.over[lane];
+                same = S.same[lane];
                 // the lanes that hold the last key to stay; all waves find the same
                 const uint64_t at = __ballot(lane < in_bin && over < need && over + same >= need);
                 const uint32_t from = __builtin_ctzll(at);
@@ -373,62 +383,70 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         }
     }
 
-    // Which stay: above, or equal and among the first.  Ties before this wave's, then before this lane's chunk by chunk.
-    uint32_t equal = 0;
-    each([&](uint32_t t, u32x4 key) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) equal += t + e < length && key[e] == least;
-    });
-    // Before the lane's first chunk: the waves before it.  (The scan's own lanes are counted chunk by chunk below.)
+    // Which stay: above, or equal and among the first.  Of the waves before this one: equal keys, then slots that come free and tokens that move.
     auto waves_before = [&](uint32_t x) {
-        uint32_t sum = wave_sum(x), before = 0;
+        const uint32_t sum = wave_sum(x);
         if (lane == 0) S.part[turn & 1][wave] = sum;
         __syncthreads();
+        uint32_t before = 0;
 #pragma unroll
         for (uint32_t v = 0; v < kSelectWaves; ++v) before += v < wave ? S.part[turn & 1][v] : 0;
         ++turn;
         return before;
     };
-    const uint32_t equal_before = waves_before(equal);
-    uint32_t ranked = equal_before, holes_mine = 0, movers_mine = 0;
-    // f(slot, bits of the four slots that stay) in order
-    auto each_kept = [&](auto f) {
-        ranked = equal_before;
-        each([&](uint32_t t, u32x4 key) {
-            uint32_t same = 0, more = 0;
+    uint32_t equal = 0;
+    each([&](uint32_t t, u32x4 key) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                same |= uint32_t(t + e < length && key[e] == least) << e;
-                more |= uint32_t(t + e < length && key[e] > least) << e;
-            }
+        for (int e = 0; e < 4; ++e) equal += t + e < length && key[e] == least;
+    });
+    const uint32_t equal_before = waves_before(equal);
+    uint32_t ranked;
+    // The bits of the four slots from t on that stay; called for the wave's chunks in order.
+    auto kept_of = [&](uint32_t t, u32x4 key) {
+        uint32_t same = 0, more = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            same |= uint32_t(t + e < length && key[e] == least) << e;
+            more |= uint32_t(t + e < length && key[e] > least) << e;
+        }
+        if (__ballot(same != 0)) {
             const uint32_t upto = wave_inclusive_scan(__popc(same));
             uint32_t rank = ranked + upto - __popc(same);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (same >> e & 1) more |= uint32_t(rank++ < ties) << e;
             ranked += __builtin_amdgcn_readlane(upto, 63);
-            f(t, more);
-        });
+        }
+        return more;
     };
-    // bits of the four slots from t on that lie below the budget, and below the length
-    auto below = [](uint32_t t, uint32_t end) { return t >= end ? 0u : end - t >= 4 ? 15u : (1u << (end - t)) - 1; };
-    each_kept([&](uint32_t t, uint32_t kept) {
-        holes_mine += __popc(below(t, budget) & ~kept);
-        movers_mine += __popc(kept & ~below(t, budget));
+    // the bits of the four slots from t on that lie below the budget
+    auto below = [&](uint32_t t) { return t >= budget ? 0u : budget - t >= 4 ? 15u : (1u << (budget - t)) - 1; };
+    ranked = equal_before;
+    uint32_t bits = 0, holes_mine = 0, movers_mine = 0, at = 0;  // bits: of all chunks, where they are registers
+    each([&](uint32_t t, u32x4 key) {
+        const uint32_t kept = kept_of(t, key);
+        bits |= kChunks ? kept << (4 * at++) : 0;
+        holes_mine += __popc(below(t) & ~kept);
+        movers_mine += __popc(kept & ~below(t));
     });
     uint32_t holes = waves_before(holes_mine), movers = waves_before(movers_mine);
     int32_t *hole_list = kMove ? S.holes : E.holes + row * E.most, *mover_list = kMove ? S.movers : E.movers + row * E.most;
-    each_kept([&](uint32_t t, uint32_t kept) {
-        const uint32_t free = below(t, budget) & ~kept, past = kept & ~below(t, budget);
-        const uint32_t f = wave_inclusive_scan(__popc(free)), m = wave_inclusive_scan(__popc(past));
-        uint32_t at = holes + f - __popc(free), to = movers + m - __popc(past);
+    ranked = equal_before;
+    at = 0;
+    each([&](uint32_t t, u32x4 key) {
+        const uint32_t kept = kChunks ? bits >> (4 * at++) & 15u : kept_of(t, key);
+        const uint32_t free = below(t) & ~kept, past = kept & ~below(t);
+        if (!__ballot((free | past) != 0)) return;
+        const uint32_t mine_of = __popc(free) | __popc(past) << 16, upto = wave_inclusive_scan(mine_of);  // at most 256 of each
+        uint32_t hole = holes + ((upto - mine_of) & 0xffffu), mover = movers + ((upto - mine_of) >> 16);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (free >> e & 1) hole_list[at++] = t + e;
-            if (past >> e & 1) mover_list[to++] = t + e;
+            if (free >> e & 1) hole_list[hole++] = t + e;
+            if (past >> e & 1) mover_list[mover++] = t + e;
         }
-        holes += __builtin_amdgcn_readlane(f, 63);
-        movers += __builtin_amdgcn_readlane(m, 63);
+        const uint32_t all = __builtin_amdgcn_readlane(upto, 63);
+        holes += all & 0xffffu;
+        movers += all >> 16;
     });
     if (threadIdx.x == kSelectThreads - 1) S.found[0] = holes;
     __threadfence_block();
@@ -438,23 +456,31 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         const int32_t to = hole_list[i], from = mover_list[i];
         w_out[to] = w[from];
         pos_out[to] = pos[from];
+        if constexpr (kMove) S.moves[i] = move_of(E.C, E.C.pages + b * E.C.pages_stride, h, to, from);
     }
-    if constexpr (kMove)
-        move_units(E.C, E.C.pages + b * E.C.pages_stride, h, hole_list, mover_list, 0, count, threadIdx.x, kSelectThreads);
-    else if (threadIdx.x == 0)
+    if constexpr (kMove) {
+        __syncthreads();
+        move_tokens(E.C, S.moves, count, kSelectThreads);
+    } else if (threadIdx.x == 0) {
         E.count[row] = count;
+    }
 }
 
-constexpr int kMovesEach = 32;  // of a workgroup of the move kernel
+constexpr int kMovesEach = 64;  // of a workgroup of the move kernel
 
 // Keys and values of the kept tokens past the budget.
 __global__ __launch_bounds__(256) void endor_kv_move_kernel(EvictParams E) {
+    __shared__ Move s_moves[kMovesEach];
     const uint32_t b = blockIdx.z, h = blockIdx.y, first = blockIdx.x * kMovesEach;
     const int64_t row = int64_t(b) * E.C.kv_heads + h;
-    const uint32_t count = E.count[row];
-    if (first >= count) return;
-    move_units(E.C, E.C.pages + b * E.C.pages_stride, h, E.holes + row * E.most, E.movers + row * E.most, first,
-               count - first < kMovesEach ? count - first : kMovesEach, threadIdx.x, 256);
+    const uint32_t all = E.count[row];
+    if (first >= all) return;
+    const uint32_t count = all - first < kMovesEach ? all - first : kMovesEach;
+    if (threadIdx.x < count)
+        s_moves[threadIdx.x] = move_of(E.C, E.C.pages + b * E.C.pages_stride, h, E.holes[row * E.most + first + threadIdx.x],
+                                       E.movers[row * E.most + first + threadIdx.x]);
+    __syncthreads();
+    move_tokens(E.C, s_moves, count, 256);
 }
 
 // The lengths in place, once nobody reads the old ones any more.
