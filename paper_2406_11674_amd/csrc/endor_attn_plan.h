@@ -7,18 +7,20 @@
 
 namespace endor_attn_plan {
 
-constexpr int kWaves = 4;       // of a workgroup
-constexpr int kTile = 32;       // slots a wave takes at a time: the inner length of the second product's instruction
-constexpr int kQueries = 16;    // query heads that share a pass over the keys: the width of an instruction's result
-constexpr int kStep = kWaves * kTile;
+constexpr int kQueries = 16;  // query heads that share a pass over the keys: the width of an instruction's result
 
 struct Plan {
     int group;           // query heads of a kv head
     int qtiles;          // passes over the keys of a kv head
-    int32_t chunk;       // slots of a workgroup
-    int32_t splits;      // workgroups over the longest sequence
-    int32_t row;         // logits of a query head kept for the weights: max_len, rounded up to whole tiles
-    size_t partial, ml, logits, bytes;  // scratch: sums of the splits, their maxima and totals, logits
+    uint32_t units;      // of a sequence: kv_heads * qtiles
+    int32_t row;         // logits of a query head: max_len, rounded up to whole tiles
+    int waves;           // of a workgroup
+    int32_t least;       // slots of a part of a sequence at least,
+    int32_t chunk;       // at most where the lengths differ,
+    int32_t even;        // and parts where they are alike: which it is the device sees
+    uint32_t heads;      // query heads that a workgroup joins
+    int32_t splits;      // parts of the longest sequence; 0: a workgroup for every unit, and no scratch
+    size_t partial, ml, logits, bytes;  // scratch: sums of parts of units, their maxima and totals, logits
 };
 
 inline size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
@@ -27,17 +29,29 @@ inline Plan make_plan(int batch, int kv_heads, int q_heads, int dim, int32_t max
     Plan p{};
     p.group = q_heads / kv_heads;
     p.qtiles = (p.group + kQueries - 1) / kQueries;
-    const int64_t units = int64_t(batch) * kv_heads * p.qtiles;
-    int64_t chunk = (int64_t(max_len) * units / 1024 + kStep - 1) / kStep * kStep;
-    if (chunk < 2 * kStep) chunk = 2 * kStep;
-    if (chunk > 1024) chunk = 1024;
+    p.units = static_cast<uint32_t>(kv_heads) * p.qtiles;
+    p.row = static_cast<int32_t>((int64_t(max_len) + 63) / 64 * 64);
+    const int64_t units = int64_t(batch) * p.units;
+    if (max_len <= 512 && units <= 512 && (p.qtiles == 1 || !with_weights)) return p;
+    // Where four waves to a compute unit would have less than two tiles each, two of them.
+    p.waves = int64_t(max_len) * units >= 256 * 256 ? 4 : 2;
+    p.least = 64 * p.waves;
+    p.even = units < 256 ? static_cast<int32_t>(256 / units) : 1;
+    // Workgroups that have no part hold up others, and a part costs what its start and its join take: some six workgroups for every compute
+    // unit (of widest heads one, for the registers of one fill it), and four tiles of 64 slots or more for two waves.
+    int64_t chunk = (int64_t(max_len) * units / (dim <= 128 ? 1536 : 256) + 63) / 64 * 64;
+    if (chunk < 2 * p.least) chunk = 2 * p.least;
+    while ((int64_t(max_len) + chunk - 1) / chunk > 65535) chunk *= 2;  // a grid's third dimension
     p.chunk = static_cast<int32_t>(chunk);
-    p.splits = static_cast<int32_t>((int64_t(max_len) + p.chunk - 1) / p.chunk);
+    p.splits = batch > 1 ? static_cast<int32_t>((int64_t(max_len) + chunk - 1) / chunk) : 1;
+    if (p.splits < p.even) p.splits = p.even;
+    const int64_t most = (int64_t(max_len) + p.least - 1) / p.least;
+    if (p.splits > most) p.splits = static_cast<int32_t>(most);
     if (p.splits < 1) p.splits = 1;
-    p.row = static_cast<int32_t>((int64_t(max_len) + kTile - 1) / kTile * kTile);
+    p.heads = p.splits <= 16 ? 8 : 1;
     const size_t rows = size_t(batch) * q_heads;
     p.partial = p.splits > 1 ? round256(rows * p.splits * dim * 4) : 0;
-    p.ml = p.splits > 1 || with_weights ? round256(rows * p.splits * 8) : 0;
+    p.ml = round256(rows * p.splits * 8);
     p.logits = with_weights ? round256(rows * p.row * 4) : 0;
     p.bytes = p.partial + p.ml + p.logits;
     return p;
