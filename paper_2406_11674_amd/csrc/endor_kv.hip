@@ -131,10 +131,10 @@ struct EvictParams {
     int32_t budget, recent, most_len, capacity, most;
 };
 
-// Weights as unsigned numbers in the same order: NaN below all, -0 with +0; what must stay above all.
+// Weights as unsigned numbers in the same order: NaN 1, below all, -0 with +0; what must stay is above all.  0 is no token.
 __device__ __forceinline__ uint32_t key_of(float w, int32_t position, int64_t newest) {
     if (position >= newest) return 0xffffffffu;
-    if (w != w) return 0;
+    if (w != w) return 1;
     const uint32_t bits = __float_as_uint(w + 0.0f);
     return bits >> 31 ? ~bits : bits | 0x80000000u;
 }
@@ -289,16 +289,14 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
 
     uint32_t turn = 0, total;
     // What stays whatever it weighs; the least and the largest key of the others.
-    uint32_t staying = 0, low = kStay, high = 0;
-    each([&](uint32_t t, u32x4 key) {
+    // One is taken off or added so that neither what stays nor what is no token is the least or the largest.
+    uint32_t staying = 0, low = 0xffffffffu, high = 0;
+    each([&](uint32_t, u32x4 key) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const bool in = t + e < length;
-            staying += in && key[e] == kStay;
-            if (in && key[e] != kStay) {
-                low = key[e] < low ? key[e] : low;
-                high = key[e] > high ? key[e] : high;
-            }
+            staying += key[e] == kStay;
+            low = key[e] - 1 < low ? key[e] - 1 : low;
+            high = key[e] + 1 > high ? key[e] + 1 : high;
         }
     });
 #pragma unroll
@@ -318,19 +316,20 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         low = S.low[v] < low ? S.low[v] : low;
         high = S.high[v] > high ? S.high[v] : high;
     }
+    ++low;
+    --high;
     uint32_t least = kStay, ties = budget;  // keys above `least` stay, and the first `ties` of those equal to it
     if (staying < budget) {
         uint32_t need = budget - staying;
         // more keys are left than are needed, so low <= high
         const uint32_t range = high - low;
         uint32_t shift = range >> kBinBits ? 32 - __clz(range) - kBinBits : 0;
-        uint64_t width = uint64_t(range) + 1;  // keys in [low, low + width) are still in question
+        uint32_t width = range + 1;  // keys in [low, low + width) are still in question: neither 0 nor what stays
         for (;;) {
-            auto in_question = [&](uint32_t t, uint32_t key) { return t < length && key != kStay && key >= low && key - low < width; };
-            each([&](uint32_t t, u32x4 key) {
+            each([&](uint32_t, u32x4 key) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (in_question(t + e, key[e])) atomicAdd(&S.bins[(key[e] - low) >> shift], 1u);
+                    if (key[e] - low < width) atomicAdd(&S.bins[(key[e] - low) >> shift], 1u);
             });
             __syncthreads();
             const uint32_t top = kBins - 1 - 2 * threadIdx.x, c0 = S.bins[top], c1 = S.bins[top - 1];
@@ -352,13 +351,13 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
                 ties = shift == 0 ? need : 0xffffffffu;  // all of the bin stay: those from its lower end on
                 break;
             }
-            width = uint64_t(1) << shift;
+            width = 1u << shift;
             shift = shift > kBinBits ? shift - kBinBits : 0;
             if (in_bin <= 64) {
-                each([&](uint32_t t, u32x4 key) {
+                each([&](uint32_t, u32x4 key) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (in_question(t + e, key[e])) S.last[atomicAdd(&S.left, 1u)] = key[e];
+                        if (key[e] - low < width) S.last[atomicAdd(&S.left, 1u)] = key[e];
                 });
                 __syncthreads();
                 const uint32_t key = lane < in_bin ? S.last[lane] : 0;
@@ -395,19 +394,19 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         return before;
     };
     uint32_t equal = 0;
-    each([&](uint32_t t, u32x4 key) {
+    each([&](uint32_t, u32x4 key) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) equal += t + e < length && key[e] == least;
+        for (int e = 0; e < 4; ++e) equal += key[e] == least;
     });
     const uint32_t equal_before = waves_before(equal);
     uint32_t ranked;
-    // The bits of the four slots from t on that stay; called for the wave's chunks in order.
-    auto kept_of = [&](uint32_t t, u32x4 key) {
+    // The bits of the four slots that stay; called for the wave's chunks in order.
+    auto kept_of = [&](u32x4 key) {
         uint32_t same = 0, more = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            same |= uint32_t(t + e < length && key[e] == least) << e;
-            more |= uint32_t(t + e < length && key[e] > least) << e;
+            same |= uint32_t(key[e] == least) << e;
+            more |= uint32_t(key[e] > least) << e;
         }
         if (__ballot(same != 0)) {
             const uint32_t upto = wave_inclusive_scan(__popc(same));
@@ -424,7 +423,7 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
     ranked = equal_before;
     uint32_t bits = 0, holes_mine = 0, movers_mine = 0, at = 0;  // bits: of all chunks, where they are registers
     each([&](uint32_t t, u32x4 key) {
-        const uint32_t kept = kept_of(t, key);
+        const uint32_t kept = kept_of(key);
         bits |= kChunks ? kept << (4 * at++) : 0;
         holes_mine += __popc(below(t) & ~kept);
         movers_mine += __popc(kept & ~below(t));
@@ -434,7 +433,7 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
     ranked = equal_before;
     at = 0;
     each([&](uint32_t t, u32x4 key) {
-        const uint32_t kept = kChunks ? bits >> (4 * at++) & 15u : kept_of(t, key);
+        const uint32_t kept = kChunks ? bits >> (4 * at++) & 15u : kept_of(key);
         const uint32_t free = below(t) & ~kept, past = kept & ~below(t);
         if (!__ballot((free | past) != 0)) return;
         const uint32_t mine_of = __popc(free) | __popc(past) << 16, upto = wave_inclusive_scan(mine_of);  // at most 256 of each
