@@ -2,7 +2,7 @@
 //
 // PACKED FORM.  Rows go in tiles of 16, columns in blocks of 128, both padded with codes and scales of zero, so that no
 // kernel has an edge in W.  Codes: [tile][block][lane 0..63][16 bytes]; lane l has row l & 15 of the tile, and its 32-bit word j the
-// columns 32 j + 8 (l >> 4) + 0..7 of the block, column c in bits 4 * kNibble[c].  Then the scales, fp16, for a tile and a block (or a
+// columns 32 j + 8 (l >> 4) + 0..7 of the block, the even ones in the lower half and the odd ones in the upper, 4 bits each.  Then the scales, fp16, for a tile and a block (or a
 // group that holds blocks): [4 quarters][groups of the block][4 rows], as the lanes of a product's result want them; then, if there
 // are any, the zeros, bytes [16 rows][groups of the block], as the lanes of its operand do.  A block and a group that holds several blocks end
 // at the same column.
@@ -61,22 +61,40 @@ struct PackParams {
     int64_t rows, cols, group, groups, tiles, blocks, padded_groups;
 };
 
-// The 4-bit place of a word's column: pairs of columns lie 16 bits apart, where packed 16-bit arithmetic takes them.
-__device__ __forceinline__ uint32_t place_of(uint32_t c) { return (c >> 1) + 4 * (c & 1); }
+// Eight columns' codes as a checkpoint has them, column c in bits 4c, with the even columns in the lower half: pairs of columns lie 16 bits
+// apart then, where packed 16-bit arithmetic takes them.
+__device__ __forceinline__ uint32_t even_below_odd(uint32_t x) {
+    auto squeeze = [](uint32_t v) {  // the low halves of four bytes side by side
+        v &= 0x0f0f0f0fu;
+        v = (v | v >> 4) & 0x00ff00ffu;
+        return (v | v >> 8) & 0xffffu;
+    };
+    return squeeze(x) | squeeze(x >> 4) << 16;
+}
 
+// A thread makes a lane's 16 bytes of a block; the first ones of a workgroup the scales and zeros.
 __global__ __launch_bounds__(256) void endor_q4_pack_kernel(PackParams P) {
-    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, words = P.tiles * P.blocks * 256;
-    if (i < words) {
-        const uint32_t j = i & 3, lane = (i >> 2) & 63;
-        const int64_t block = (i >> 8) % P.blocks, row = (i >> 8) / P.blocks * 16 + (lane & 15), col = block * 128 + 32 * j + 8 * (lane >> 4);
-        uint32_t word = 0;
-        if (row < P.rows)
-            for (uint32_t c = 0; c < 8; ++c)
-                if (col + c < P.cols) {
-                    const uint32_t two = P.codes[row * ((P.cols + 1) / 2) + (col + c) / 2];
-                    word |= ((c & 1) ? two >> 4 : two & 15u) << (4 * place_of(c));  // col is even
+    const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, units = P.tiles * P.blocks * 64;
+    if (i < units) {
+        const uint32_t lane = i & 63;
+        const int64_t block = (i >> 6) % P.blocks, row = (i >> 6) / P.blocks * 16 + (lane & 15), pitch = (P.cols + 1) / 2;
+        u32x4 words = {0, 0, 0, 0};
+        if (row < P.rows) {
+            const uint8_t *from = P.codes + row * pitch;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t col = block * 128 + 32 * j + 8 * (lane >> 4);
+                uint32_t x = 0;
+                if (col + 8 <= P.cols) {
+                    typedef uint32_t u32_any __attribute__((aligned(1)));
+                    x = *reinterpret_cast<const u32_any *>(from + col / 2);
+                } else {
+                    for (int64_t c = col; c < P.cols; ++c) x |= ((c & 1 ? from[c / 2] >> 4 : from[c / 2] & 15u)) << (4 * (c - col));  // col is even
                 }
-        P.out_codes[i] = word;
+                words[j] = even_below_odd(x);
+            }
+        }
+        reinterpret_cast<u32x4 *>(P.out_codes)[i] = words;
     }
     const int64_t entries = P.tiles * P.padded_groups * 16;
     if (i < entries) {
@@ -427,8 +445,8 @@ extern "C" endor_status endor_q4_pack(int64_t rows, int64_t cols, int group, con
     P.tiles = l.tiles;
     P.blocks = l.blocks;
     P.padded_groups = l.groups;
-    // 256 words of codes a tile and block, and at most 64 scales
-    hipLaunchKernelGGL(endor_q4_pack_kernel, dim3(static_cast<uint32_t>(l.tiles * l.blocks)), dim3(256), 0, static_cast<hipStream_t>(stream), P);
+    // 64 units of codes a tile and block, and at most 64 scales
+    hipLaunchKernelGGL(endor_q4_pack_kernel, dim3(static_cast<uint32_t>((l.tiles * l.blocks + 3) / 4)), dim3(256), 0, static_cast<hipStream_t>(stream), P);
     return hipGetLastError() == hipSuccess ? ENDOR_OK : ENDOR_ERR_HIP;
 }
 
