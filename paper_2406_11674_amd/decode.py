@@ -2,6 +2,7 @@
 4-bit weights.  Argument marshalling over include/endor.h, as in `binding`; every step runs inside libendor.so."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from dataclasses import dataclass
 
@@ -47,6 +48,11 @@ def _lib():
 
 # The checks of a call are on the way of every token, and a tensor's attributes take 50 ns each: they are asked for
 # once, tensor by tensor, and not through helpers (an append took 10 us of the host with those, the kernel 4).
+
+def _of(stream):
+    """What a call allocates, copies or clears for itself belongs to the stream that its kernels run on."""
+    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+
 
 def _bad(what):
     raise ValueError(what)
@@ -135,14 +141,15 @@ def kv_append(cache, k, v, lengths, seen=None, counts=None, weights=None, positi
         _bad("k and v must be [batch, tokens, kv_heads, head_dim] of the cache")
     st = k.stride()
     if v.stride() != st or st[3] != 1:
-        k, v = k.contiguous(), v.contiguous()
+        with _of(stream):
+            k, v = k.contiguous(), v.contiguous()
         st = k.stride()
     if seen is None:
         seen = lengths
-    if new_lengths is None:
-        new_lengths = torch.empty_like(lengths)
-    if new_seen is None:
-        new_seen = torch.empty_like(seen)
+    if new_lengths is None or new_seen is None:
+        with _of(stream):
+            new_lengths = torch.empty_like(lengths) if new_lengths is None else new_lengths
+            new_seen = torch.empty_like(seen) if new_seen is None else new_seen
     cache._per_sequence(lengths, seen, new_lengths, new_seen)
     if counts is not None:
         cache._per_sequence(counts)
@@ -186,16 +193,18 @@ def attn_decode(cache, q, lengths, max_len=None, mask=None, scale=None, weights=
         _bad("weights without new_weights: pass the buffer for the sums, which may be weights itself")
     if new_weights is not None:
         cache._per_slot(torch.float32, weights, new_weights)
-    if out is None:
-        out = torch.empty((batch, q_heads, cache.head_dim), dtype=q.dtype, device=q.device)
-    elif out.dtype is not cache.dtype or out.shape != shape or out.get_device() != device or not out.is_contiguous():
+    if out is None or lse is None or scratch is None:
+        with _of(stream):
+            if out is None:
+                out = torch.empty((batch, q_heads, cache.head_dim), dtype=q.dtype, device=q.device)
+            if lse is None:
+                lse = torch.empty((batch, q_heads), dtype=torch.float32, device=q.device)
+            if scratch is None:
+                scratch = cache.attn_scratch(q_heads, max_len, new_weights is not None)
+    if out.dtype is not cache.dtype or out.shape != shape or out.get_device() != device or not out.is_contiguous():
         _bad("out must be a contiguous tensor like q")
-    if lse is None:
-        lse = torch.empty((batch, q_heads), dtype=torch.float32, device=q.device)
-    elif lse.dtype is not torch.float32 or lse.numel() != batch * q_heads or lse.get_device() != device or not lse.is_contiguous():
+    if lse.dtype is not torch.float32 or lse.numel() != batch * q_heads or lse.get_device() != device or not lse.is_contiguous():
         _bad("lse must be a contiguous float32 tensor [batch, q_heads]")
-    if scratch is None:
-        scratch = cache.attn_scratch(q_heads, max_len, new_weights is not None)
     scratch_at, room = cache._take(scratch)
     status = _lib().endor_attn_decode(cache._at, q_heads, q.data_ptr(), st[0], st[1], lengths.data_ptr(), max_len, mask_at, mask_stride,
                                       cache.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr(),
@@ -212,14 +221,16 @@ def kv_evict(cache, lengths, seen, weights, positions, budget, recent, max_len=N
     Returns (new_lengths, new_weights, new_positions); pass the inputs for them to change in place."""
     torch = _torch()
     max_len = cache.capacity if max_len is None else max_len
-    new_lengths = torch.empty_like(lengths) if new_lengths is None else new_lengths
-    new_weights = torch.zeros_like(weights) if new_weights is None else new_weights
-    new_positions = torch.zeros_like(positions) if new_positions is None else new_positions
+    if new_lengths is None or new_weights is None or new_positions is None or scratch is None:
+        with _of(stream):
+            new_lengths = torch.empty_like(lengths) if new_lengths is None else new_lengths
+            new_weights = torch.zeros_like(weights) if new_weights is None else new_weights
+            new_positions = torch.zeros_like(positions) if new_positions is None else new_positions
+            if scratch is None:
+                scratch = cache.evict_scratch(budget, max_len)
     cache._per_sequence(lengths, seen, new_lengths)
     cache._per_slot(torch.float32, weights, new_weights)
     cache._per_slot(torch.int32, positions, new_positions)
-    if scratch is None:
-        scratch = cache.evict_scratch(budget, max_len)
     scratch_at, room = cache._take(scratch)
     status = _lib().endor_kv_evict(cache._at, budget, recent, max_len, lengths.data_ptr(), seen.data_ptr(), weights.data_ptr(), positions.data_ptr(),
                                    new_lengths.data_ptr(), new_weights.data_ptr(), new_positions.data_ptr(), scratch_at, room,
@@ -264,7 +275,8 @@ def q4_pack(codes, scales, zeros, cols, group, stream=None):
     if any(t is not None and t.get_device() != codes.get_device() for t in (scales, zeros)):
         raise ValueError("codes, scales and zeros must be on one GPU")
     L = _lib()
-    packed = torch.empty(L.endor_q4_bytes(rows, cols, group, int(zeros is not None)), dtype=torch.uint8, device=codes.device)
+    with _of(stream):
+        packed = torch.empty(L.endor_q4_bytes(rows, cols, group, int(zeros is not None)), dtype=torch.uint8, device=codes.device)
     _check(L.endor_q4_pack(rows, cols, group, _dptr(codes), _dptr(scales), _dptr(zeros), _dptr(packed), packed.numel(), _stream_handle(stream)),
            "endor_q4_pack")
     return Q4Matrix(rows, cols, group, zeros is not None, packed)
@@ -280,9 +292,10 @@ def q4_quantize(dense, group=128, zeros=False, stream=None):
         raise ValueError("dense must lie in GPU memory")
     if group < 1:
         raise ValueError("group must be a power of two from 32 on")
-    codes = torch.empty((rows, (cols + 1) // 2), dtype=torch.uint8, device=dense.device)
-    scales = torch.empty((rows, _q4_groups(cols, group)), dtype=torch.float16, device=dense.device)
-    points = torch.empty(scales.shape, dtype=torch.uint8, device=dense.device) if zeros else None
+    with _of(stream):
+        codes = torch.empty((rows, (cols + 1) // 2), dtype=torch.uint8, device=dense.device)
+        scales = torch.empty((rows, _q4_groups(cols, group)), dtype=torch.float16, device=dense.device)
+        points = torch.empty(scales.shape, dtype=torch.uint8, device=dense.device) if zeros else None
     _check(_lib().endor_q4_quantize(rows, cols, group, _dptr(dense), _dptr(codes), _dptr(scales), _dptr(points), _stream_handle(stream)),
            "endor_q4_quantize")
     return codes, scales, points
@@ -303,7 +316,8 @@ def q4_gemm(m, X, Y=None, scratch=None, stream=None):
     if inner != 1 and m.cols > 1:
         _bad("X must have contiguous rows")
     if Y is None:
-        Y = torch.empty((nb, rows), dtype=torch.float32, device=X.device)
+        with _of(stream):
+            Y = torch.empty((nb, rows), dtype=torch.float32, device=X.device)
     elif Y.dtype is not torch.float32 or Y.numel() != nb * rows or Y.get_device() != device or not Y.is_contiguous():
         _bad("Y must be a contiguous fp32 tensor of nb*rows elements, on the weight's GPU")
     L = _lib()
@@ -311,7 +325,8 @@ def q4_gemm(m, X, Y=None, scratch=None, stream=None):
     if scratch is None:
         room = L.endor_q4_scratch_bytes(rows, m.cols, m.group, nb)
         if room:
-            scratch = torch.empty(room, dtype=torch.uint8, device=X.device)
+            with _of(stream):
+                scratch = torch.empty(room, dtype=torch.uint8, device=X.device)
     elif scratch.get_device() != device or not scratch.is_contiguous():
         _bad("scratch must be contiguous, on the weight's GPU")
     if scratch is not None:

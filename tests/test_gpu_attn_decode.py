@@ -237,25 +237,6 @@ def test_offsets_past_32_bits():
     check(endor.KVCache(kd, vd, torch.from_numpy(table).cuda()), q, k.float().numpy(), v.float().numpy(), table, [60], torch.float16)
 
 
-def test_same_from_run_to_run_and_on_another_stream():
-    lengths = [3000, 17, 900]
-    cache, q, k, v, table = make(lengths, (32, 4), 128, 16, torch.bfloat16, seed=14)
-    qd, lens = q.cuda(), torch.tensor(lengths, dtype=torch.int32, device="cuda")
-    first = endor.attn_decode(cache, qd, lens)
-    torch.cuda.synchronize()
-    side = torch.cuda.Stream()
-    scratch = cache.attn_scratch(32)
-    with torch.cuda.stream(side):
-        torch.cuda._sleep(1000000)
-        late = qd * 1  # made on the side stream after a while
-        second = endor.attn_decode(cache, late, lens, scratch=scratch)
-    side.synchronize()
-    third = endor.attn_decode(cache, qd, lens, stream=side)
-    side.synchronize()
-    for other in (second, third):
-        assert torch.equal(first[0], other[0]) and torch.equal(first[1], other[1])
-
-
 def test_refusals():
     lengths = [20]
     cache, q, *_ = make(lengths, (4, 2), 64, 16, torch.float16)

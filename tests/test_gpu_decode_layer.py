@@ -1,5 +1,4 @@
-"""The decode side as it is used together: the example's attention block step by step against the oracle, its eviction included, and
-steps replayed from a HIP graph while lengths grow on the GPU."""
+"""The decode side as it is used together: the example's attention block step by step against the oracle, its eviction included."""
 import importlib.util
 import os
 
@@ -38,7 +37,7 @@ def test_the_example_against_the_oracle():
         w, pos = layer.weights.cpu().numpy().copy(), layer.positions.cpu().numpy().copy()
         x = torch.randn((3, 512), generator=g, device="cuda").half()
         caught = {}
-        attend, drop = endor.attn_decode, endor.kv_evict
+        attend = endor.attn_decode
 
         def attn_decode(cache, q, *args, **kw):
             caught["q"] = q.clone()
@@ -54,11 +53,9 @@ def test_the_example_against_the_oracle():
             endor.attn_decode = attend
         torch.cuda.synchronize()
         q = caught["q"]
-        # the projections, from what the cache was given
-        dense = layer.wk.m
+        # the key projection, from what the cache was given
         new = np.stack([caught["k"].cpu().numpy()[table[b, lengths[b] // 16], :, lengths[b] % 16] for b in range(3)])
         newv = np.stack([caught["v"].cpu().numpy()[table[b, lengths[b] // 16], :, lengths[b] % 16] for b in range(3)])
-        assert dense.rows == 128
         ref_k = endor.q4_gemm(layer.wk.m, x).half().view(3, 2, 64).cpu().numpy()
         assert np.array_equal(new, ref_k)
         lengths, seen = orc.append(k, v, table, lengths, seen, new[:, None], newv[:, None], None, w, pos)
@@ -79,58 +76,3 @@ def test_the_example_against_the_oracle():
             assert np.array_equal(layer.weights.cpu().numpy()[b, :, :after[b]], w[b, :, :after[b]])
             assert np.array_equal(layer.positions.cpu().numpy()[b, :, :after[b]], pos[b, :, :after[b]])
         assert torch.isfinite(y.float()).all()
-    assert drop is endor.kv_evict
-
-
-def state(batch, kv, dim, page, pages, seed):
-    g = torch.Generator(device="cuda").manual_seed(seed)
-    table = torch.randperm(batch * pages, generator=g, device="cuda").to(torch.int32).view(batch, pages)
-    pool = torch.zeros((2, batch * pages, kv, page, dim), dtype=torch.bfloat16, device="cuda")
-    cache = endor.KVCache(pool[0], pool[1], table)
-    return {"cache": cache, "pool": pool, "lengths": torch.tensor([0, 17, 300][:batch], dtype=torch.int32, device="cuda"),
-            "seen": torch.tensor([0, 17, 300][:batch], dtype=torch.int32, device="cuda"),
-            "weights": torch.zeros((batch, kv, cache.capacity), device="cuda"),
-            "positions": torch.arange(cache.capacity, dtype=torch.int32, device="cuda").expand(batch, kv, cache.capacity).contiguous(),
-            "out": torch.zeros((batch, 4 * kv, dim), dtype=torch.bfloat16, device="cuda"), "lse": torch.zeros((batch, 4 * kv), device="cuda"),
-            "x": torch.zeros((batch, 6 * kv, dim), dtype=torch.bfloat16, device="cuda"),
-            "scratch": cache.attn_scratch(4 * kv, weights=True), "drop": cache.evict_scratch(310)}
-
-
-def one_step(s, kv, most):
-    q, k, v = s["x"][:, :4 * kv], s["x"][:, 4 * kv:5 * kv], s["x"][:, 5 * kv:]
-    endor.kv_append(s["cache"], k, v, s["lengths"], s["seen"], weights=s["weights"], positions=s["positions"], new_lengths=s["lengths"], new_seen=s["seen"])
-    endor.attn_decode(s["cache"], q, s["lengths"], max_len=most, weights=s["weights"], new_weights=s["weights"], out=s["out"], lse=s["lse"],
-                      scratch=s["scratch"])
-    endor.kv_evict(s["cache"], s["lengths"], s["seen"], s["weights"], s["positions"], 310, 16, new_lengths=s["lengths"], new_weights=s["weights"],
-                   new_positions=s["positions"], scratch=s["drop"])
-
-
-@pytest.mark.parametrize("most", [400, 2048], ids=["one launch", "parts"])
-def test_steps_in_a_hip_graph(most):
-    """Replays with the program's own work and synchronizations in between give what eager calls give, bit for bit, while lengths
-    grow and one sequence passes its budget."""
-    kv, dim = 2, 64
-    eager, graphed = (state(3, kv, dim, 16, 128, 9) for _ in range(2))
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
-    warm = state(3, kv, dim, 16, 128, 10)
-    with torch.cuda.stream(side):
-        one_step(warm, kv, most)
-    torch.cuda.current_stream().wait_stream(side)
-    torch.cuda.synchronize()
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph, stream=side):
-        one_step(graphed, kv, most)
-    g = torch.Generator(device="cuda").manual_seed(11)
-    for step in range(25):
-        x = torch.randn(eager["x"].shape, generator=g, device="cuda").bfloat16()
-        eager["x"].copy_(x)
-        graphed["x"].copy_(x)
-        if step % 3 == 0:
-            torch.cuda.synchronize()
-        one_step(eager, kv, most)
-        graph.replay()
-        torch.cuda.synchronize()
-        for name in ("pool", "lengths", "seen", "weights", "positions", "out", "lse"):
-            assert torch.equal(eager[name], graphed[name]), (step, name)
-    assert eager["lengths"].tolist() == [25, 42, 310] and eager["seen"].tolist() == [25, 42, 325]

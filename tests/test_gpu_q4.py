@@ -137,17 +137,6 @@ def test_not_finite_inputs():
     assert np.array_equal(np.isnan(y[2]), np.isnan(ref[2])) and np.array_equal(np.isinf(y[2]), np.isinf(ref[2]))
 
 
-def test_same_from_run_to_run():
-    m, w, g = make(300, 5000, 128, True, seed=6)
-    x = torch.from_numpy(g.standard_normal((16, 5000), dtype=np.float32)).half().cuda()
-    a = endor.q4_gemm(m, x)
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
-    b = endor.q4_gemm(m, x, stream=side)
-    side.synchronize()
-    assert torch.equal(a, b)
-
-
 def test_empty():
     m, w, g = make(5, 64, 32, True)
     assert endor.q4_gemm(m, torch.zeros((0, 64), dtype=torch.float16, device="cuda")).shape == (0, 5)
