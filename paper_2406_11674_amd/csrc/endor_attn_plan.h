@@ -32,7 +32,7 @@ inline Plan make_plan(int batch, int kv_heads, int q_heads, int dim, int32_t max
     p.units = static_cast<uint32_t>(kv_heads) * p.qtiles;
     p.row = static_cast<int32_t>((int64_t(max_len) + 63) / 64 * 64);
     const int64_t units = int64_t(batch) * p.units;
-// One launch where a compute unit reads its share in about the time of the second one (1024 slots of one head of 64, or 512 of 128: 8.6 us in one
+    // One launch where a compute unit reads its share in about the time of the second one (1024 slots of one head of 64, or 512 of 128: 8.6 us in one
     // launch, 8.8 in two; 1024 of 128 17.8 and 10.8), or where the units fill half of the chip by themselves (256 of 1000 slots: 24.7 and 29.5).
     if (max_len <= 1024 && units <= 512 && (int64_t(max_len) * dim <= 65536 || units >= 128) && (p.qtiles == 1 || !with_weights)) return p;
     // Where four waves to a compute unit would have less than two tiles each, two of them.
@@ -41,7 +41,9 @@ inline Plan make_plan(int batch, int kv_heads, int q_heads, int dim, int32_t max
     p.even = units < 256 ? static_cast<int32_t>(256 / units) : 1;
     // Workgroups that have no part hold up others, and a part costs what its start and its join take: some six workgroups for every compute
     // unit (of widest heads one, for the registers of one fill it), and four tiles of 64 slots or more for two waves.
-    int64_t chunk = (int64_t(max_len) * units / (dim <= 128 ? 1536 : 256) + 63) / 64 * 64;
+    const int64_t groups = dim <= 128 ? 1536 : 256;
+    int64_t chunk = ((int64_t(max_len) * units + groups - 1) / groups + 63) / 64 * 64;
+    if (chunk > p.row) chunk = p.row;
     if (chunk < 2 * p.least) chunk = 2 * p.least;
     while ((int64_t(max_len) + chunk - 1) / chunk > 65535) chunk *= 2;  // a grid's third dimension
     p.chunk = static_cast<int32_t>(chunk);
@@ -51,9 +53,13 @@ inline Plan make_plan(int batch, int kv_heads, int q_heads, int dim, int32_t max
     if (p.splits > most) p.splits = static_cast<int32_t>(most);
     if (p.splits < 1) p.splits = 1;
     p.heads = p.splits <= 16 ? 8 : 1;
+    // Scratch is what the largest plan up to max_len takes, so that scratch for a bound serves every lower one too.
+    const int64_t ceiling = (groups + units - 1) / units;
+    int64_t parts = (int64_t(max_len) + 127) / 128;
+    if (parts > (ceiling > p.even ? ceiling : p.even)) parts = ceiling > p.even ? ceiling : p.even;
     const size_t rows = size_t(batch) * q_heads;
-    p.partial = p.splits > 1 ? round256(rows * p.splits * dim * 4) : 0;
-    p.ml = round256(rows * p.splits * 8);
+    p.partial = parts > 1 ? round256(rows * parts * dim * 4) : 0;
+    p.ml = round256(rows * parts * 8);
     p.logits = with_weights ? round256(rows * p.row * 4) : 0;
     p.bytes = p.partial + p.ml + p.logits;
     return p;

@@ -7,7 +7,7 @@ import ctypes
 from dataclasses import dataclass
 
 from . import binding
-from .binding import _check, _dptr, _i64, _p, _stream_handle, _sz, _torch
+from .binding import _check, _dptr, _i64, _p, _sz
 
 __all__ = ["KVCache", "kv_append", "attn_decode", "kv_evict", "Q4Matrix", "q4_pack", "q4_quantize", "q4_scratch_bytes", "q4_gemm"]
 
@@ -21,12 +21,22 @@ class _Cache(ctypes.Structure):
 
 
 _lib_declared = None
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _lib():
     global _lib_declared
-    L = binding.lib()
-    if _lib_declared is not L:
+    L = binding._lib
+    if L is None or _lib_declared is not L:
+        L = binding.lib()
         for name, args in (
                 ("endor_kv_append", [_p, _p, _p, _i64, _i64, _i64, ctypes.c_int, _p, _p, _p, _p, _p, _p, _p, _p]),
                 ("endor_attn_decode", [_p, ctypes.c_int, _p, _i64, _i64, _p, _i32, _p, _i64, ctypes.c_float, _p, _p, _p, _p, _p, _sz, _p]),
@@ -44,6 +54,16 @@ def _lib():
             getattr(L, name).argtypes = args
         _lib_declared = L
     return L
+
+
+def _stream(stream, device):
+    """The handle of the stream that a call goes to: the given one, or the current one of the tensors' GPU."""
+    if stream is not None:
+        return stream.cuda_stream
+    try:
+        return _torch_module._C._cuda_getCurrentRawStream(device)  # not part of torch's interface: 0.2 us for 2.9
+    except AttributeError:
+        return int(_torch().cuda.current_stream(device).cuda_stream)
 
 
 # The checks of a call are on the way of every token, and a tensor's attributes take 50 ns each: they are asked for
@@ -108,7 +128,7 @@ class KVCache:
         return self._scratch(_lib().endor_kv_evict_scratch_bytes(self._at, budget, self.capacity if max_len is None else max_len))
 
     def _per_sequence(self, *tensors):
-        i32, batch, device = _torch().int32, self.batch, self.device_index
+        i32, batch, device = _torch_module.int32, self.batch, self.device_index
         for t in tensors:
             if t.dtype is not i32 or t.get_device() != device or t.numel() != batch or not t.is_contiguous():
                 _bad("lengths, seen, counts and what they become must be contiguous int32 tensors [batch] on the cache's GPU")
@@ -160,7 +180,7 @@ def kv_append(cache, k, v, lengths, seen=None, counts=None, weights=None, positi
     status = _lib().endor_kv_append(cache._at, k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], tokens, None if counts is None else counts.data_ptr(),
                                     lengths.data_ptr(), seen.data_ptr(), new_lengths.data_ptr(), new_seen.data_ptr(),
                                     None if weights is None else weights.data_ptr(), None if positions is None else positions.data_ptr(),
-                                    _stream_handle(stream))
+                                    _stream(stream, device))
     if status:
         _check(status, "endor_kv_append")
     return new_lengths, new_seen
@@ -209,7 +229,7 @@ def attn_decode(cache, q, lengths, max_len=None, mask=None, scale=None, weights=
     status = _lib().endor_attn_decode(cache._at, q_heads, q.data_ptr(), st[0], st[1], lengths.data_ptr(), max_len, mask_at, mask_stride,
                                       cache.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr(),
                                       None if weights is None else weights.data_ptr(), None if new_weights is None else new_weights.data_ptr(),
-                                      scratch_at, room, _stream_handle(stream))
+                                      scratch_at, room, _stream(stream, device))
     if status:
         _check(status, "endor_attn_decode")
     return out, lse
@@ -234,7 +254,7 @@ def kv_evict(cache, lengths, seen, weights, positions, budget, recent, max_len=N
     scratch_at, room = cache._take(scratch)
     status = _lib().endor_kv_evict(cache._at, budget, recent, max_len, lengths.data_ptr(), seen.data_ptr(), weights.data_ptr(), positions.data_ptr(),
                                    new_lengths.data_ptr(), new_weights.data_ptr(), new_positions.data_ptr(), scratch_at, room,
-                                   _stream_handle(stream))
+                                   _stream(stream, cache.device_index))
     if status:
         _check(status, "endor_kv_evict")
     return new_lengths, new_weights, new_positions
@@ -249,7 +269,11 @@ class Q4Matrix:
     cols: int
     group: int
     zeros: bool     # whether it has zero points of its own
-    packed: object  # torch.uint8
+    packed: object  # torch.uint8, the tensor of q4_pack
+
+    def __post_init__(self):
+        self._packed = (self.packed.data_ptr(), self.packed.numel(), self.packed.get_device())
+        self._scratch = {}  # bytes by the number of right-hand sides: a plan's figures, asked for once
 
 
 def _q4_groups(cols, group):
@@ -277,7 +301,7 @@ def q4_pack(codes, scales, zeros, cols, group, stream=None):
     L = _lib()
     with _of(stream):
         packed = torch.empty(L.endor_q4_bytes(rows, cols, group, int(zeros is not None)), dtype=torch.uint8, device=codes.device)
-    _check(L.endor_q4_pack(rows, cols, group, _dptr(codes), _dptr(scales), _dptr(zeros), _dptr(packed), packed.numel(), _stream_handle(stream)),
+    _check(L.endor_q4_pack(rows, cols, group, _dptr(codes), _dptr(scales), _dptr(zeros), _dptr(packed), packed.numel(), _stream(stream, codes.get_device())),
            "endor_q4_pack")
     return Q4Matrix(rows, cols, group, zeros is not None, packed)
 
@@ -296,43 +320,43 @@ def q4_quantize(dense, group=128, zeros=False, stream=None):
         codes = torch.empty((rows, (cols + 1) // 2), dtype=torch.uint8, device=dense.device)
         scales = torch.empty((rows, _q4_groups(cols, group)), dtype=torch.float16, device=dense.device)
         points = torch.empty(scales.shape, dtype=torch.uint8, device=dense.device) if zeros else None
-    _check(_lib().endor_q4_quantize(rows, cols, group, _dptr(dense), _dptr(codes), _dptr(scales), _dptr(points), _stream_handle(stream)),
+    _check(_lib().endor_q4_quantize(rows, cols, group, _dptr(dense), _dptr(codes), _dptr(scales), _dptr(points), _stream(stream, dense.get_device())),
            "endor_q4_quantize")
     return codes, scales, points
 
 
 def q4_scratch_bytes(m, nb):
     """endor_q4_scratch_bytes: scratch of q4_gemm with that many right-hand sides; mostly none."""
-    return int(_lib().endor_q4_scratch_bytes(m.rows, m.cols, m.group, nb))
+    need = m._scratch.get(nb)
+    if need is None:
+        need = m._scratch[nb] = int(_lib().endor_q4_scratch_bytes(m.rows, m.cols, m.group, nb))
+    return need
 
 
 def q4_gemm(m, X, Y=None, scratch=None, stream=None):
     """endor_q4_gemm: Y (fp32, nb x rows) = X W^T; X: (nb, cols) float16 or bfloat16 (row stride = ldx), nb <= 16."""
-    torch = _torch()
-    shape, rows, device = X.shape, m.rows, m.packed.get_device()
-    if len(shape) != 2 or shape[1] != m.cols or X.get_device() != device:
-        _bad("X must be (nb, cols), on the weight's GPU")
-    nb, (ldx, inner) = shape[0], X.stride()
-    if inner != 1 and m.cols > 1:
-        _bad("X must have contiguous rows")
+    torch, dtype = _torch(), X.dtype
+    at, room, device = m._packed
+    (nb, cols), (ldx, inner), rows = X.shape, X.stride(), m.rows  # a ValueError if X is not a matrix
+    if cols != m.cols or X.get_device() != device or (inner != 1 and cols > 1):
+        _bad("X must be (nb, cols) with contiguous rows, on the weight's GPU")
     if Y is None:
         with _of(stream):
             Y = torch.empty((nb, rows), dtype=torch.float32, device=X.device)
     elif Y.dtype is not torch.float32 or Y.numel() != nb * rows or Y.get_device() != device or not Y.is_contiguous():
         _bad("Y must be a contiguous fp32 tensor of nb*rows elements, on the weight's GPU")
-    L = _lib()
-    scratch_at, room = None, 0
+    scratch_at, space = None, 0
     if scratch is None:
-        room = L.endor_q4_scratch_bytes(rows, m.cols, m.group, nb)
-        if room:
+        need = q4_scratch_bytes(m, nb)
+        if need:
             with _of(stream):
-                scratch = torch.empty(room, dtype=torch.uint8, device=X.device)
+                scratch = torch.empty(need, dtype=torch.uint8, device=X.device)
     elif scratch.get_device() != device or not scratch.is_contiguous():
         _bad("scratch must be contiguous, on the weight's GPU")
     if scratch is not None:
-        scratch_at, room = scratch.data_ptr(), scratch.numel() * scratch.element_size()
-    status = L.endor_q4_gemm(rows, m.cols, m.group, m.zeros, m.packed.data_ptr(), m.packed.numel(), _dtype_code(X.dtype), X.data_ptr(),
-                             ldx if nb > 1 else m.cols, nb, Y.data_ptr(), scratch_at, room, _stream_handle(stream))
+        scratch_at, space = scratch.data_ptr(), scratch.numel() * scratch.element_size()
+    status = _lib().endor_q4_gemm(rows, cols, m.group, m.zeros, at, room, 0 if dtype is torch.float16 else _dtype_code(dtype), X.data_ptr(),
+                                  ldx if nb > 1 else cols, nb, Y.data_ptr(), scratch_at, space, _stream(stream, device))
     if status:
         _check(status, "endor_q4_gemm")
     return Y
