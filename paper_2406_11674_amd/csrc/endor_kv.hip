@@ -139,9 +139,8 @@ __device__ __forceinline__ uint32_t key_of(float w, int32_t position, int64_t ne
     return bits >> 31 ? ~bits : bits | 0x80000000u;
 }
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kMostWaves = 16;                       // of a workgroup that selects
 constexpr int kBinBits = 11, kBins = 1 << kBinBits;  // of a pass over the keys
-static_assert(kBins == 2 * kSelectThreads, "a thread reads two bins");
 
 // Where a token's keys and values are and go: element offsets from the pools' beginnings; -1 where a page is not there.
 struct Move {
@@ -158,8 +157,8 @@ constexpr int kFewMoves = 64;
 
 struct SelectShared {
     uint32_t bins[kBins];
-    uint32_t part[2][kSelectWaves];
-    uint32_t low[kSelectWaves], high[kSelectWaves];
+    uint32_t part[2][kMostWaves];
+    uint32_t low[kMostWaves], high[kMostWaves];
     uint32_t found[3];  // the bin that the last kept key is in, the keys above it, the keys in it
     uint32_t left, last[64], over[64], same[64];  // the keys in question, when a wave can hold them; the keys above each and its equals
     int32_t holes[kFewMoves], movers[kFewMoves];
@@ -167,6 +166,7 @@ struct SelectShared {
 };
 
 // Exclusive prefix over the workgroup, and the total.  `turn` changes from one call to the next, so that one barrier does.
+template <uint32_t kWaves>
 __device__ __forceinline__ uint32_t group_scan(uint32_t x, SelectShared &S, uint32_t turn, uint32_t *total) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t upto = wave_inclusive_scan(x);
@@ -174,7 +174,7 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t x, SelectShared &S, uint
     __syncthreads();
     uint32_t before = 0, sum = 0;
 #pragma unroll
-    for (uint32_t w = 0; w < kSelectWaves; ++w) {
+    for (uint32_t w = 0; w < kWaves; ++w) {
         before += w < wave ? S.part[turn & 1][w] : 0;
         sum += S.part[turn & 1][w];
     }
@@ -212,8 +212,10 @@ __device__ __forceinline__ void move_tokens(const Cache &C, const Move *moves, u
 // time, four to a lane: loads are whole lines, and ranks in the order of slots need wave scans only.  kChunks: such chunks of a wave that it
 // keeps as keys in registers; 0: the keys are formed anew in every pass, for rows past 32768 slots.
 // kMove: the moves are few and done here.
-template <int kChunks, bool kMove>
-__global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictParams E) {
+template <int kThreads, int kChunks, bool kMove>
+__global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E) {
+    constexpr uint32_t kWaves = kThreads / 64;
+    constexpr int kOwn = kBins / kThreads;  // bins that a thread reads
     __shared__ SelectShared S;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t b = blockIdx.y, h = blockIdx.x;
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
     if (length <= budget || budget == 0) {
         const uint32_t kept = length < budget ? length : budget;
         if (copies)
-            for (uint32_t t = threadIdx.x; t < kept; t += kSelectThreads) {
+            for (uint32_t t = threadIdx.x; t < kept; t += kThreads) {
                 w_out[t] = w[t];
                 pos_out[t] = pos[t];
             }
@@ -236,7 +238,7 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         return;
     }
     const int64_t newest = int64_t(E.seen[b]) - E.recent;
-    const uint32_t chunks = kChunks ? kChunks : (length + 256 * kSelectWaves - 1) / (256 * kSelectWaves);
+    const uint32_t chunks = kChunks ? kChunks : (length + 256 * kWaves - 1) / (256 * kWaves);
     const uint32_t mine = wave * chunks * 256 + 4 * lane;  // slot of this lane's first key
     typedef f32x4 f32x4_any __attribute__((aligned(4)));
     typedef i32x4 i32x4_any __attribute__((aligned(4)));
@@ -256,8 +258,8 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         }
         return key;
     };
-    S.bins[threadIdx.x] = 0;
-    S.bins[threadIdx.x + kSelectThreads] = 0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) S.bins[threadIdx.x + i * kThreads] = 0;
     if (threadIdx.x < 64) S.over[threadIdx.x] = S.same[threadIdx.x] = 0;
     if (threadIdx.x == 0) S.left = 0;
     u32x4 held[kChunks ? kChunks : 1];
@@ -309,10 +311,10 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         S.low[wave] = low;
         S.high[wave] = high;
     }
-    group_scan(staying, S, turn++, &total);  // its barrier is for both
+    group_scan<kWaves>(staying, S, turn++, &total);  // its barrier is for both
     staying = total;
 #pragma unroll
-    for (int v = 0; v < kSelectWaves; ++v) {
+    for (uint32_t v = 0; v < kWaves; ++v) {
         low = S.low[v] < low ? S.low[v] : low;
         high = S.high[v] > high ? S.high[v] : high;
     }
@@ -332,16 +334,26 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
                     if (key[e] - low < width) atomicAdd(&S.bins[(key[e] - low) >> shift], 1u);
             });
             __syncthreads();
-            const uint32_t top = kBins - 1 - 2 * threadIdx.x, c0 = S.bins[top], c1 = S.bins[top - 1];
-            S.bins[top] = 0;
-            S.bins[top - 1] = 0;
-            const uint32_t above = group_scan(c0 + c1, S, turn++, &total);
-            if (above < need && above + c0 + c1 >= need) {
-                const bool second = above + c0 < need;
-                S.found[0] = second ? top - 1 : top;
-                S.found[1] = second ? above + c0 : above;
-                S.found[2] = second ? c1 : c0;
+            // from the top down
+            const uint32_t top = kBins - 1 - kOwn * threadIdx.x;
+            uint32_t own[kOwn], sum = 0;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                own[i] = S.bins[top - i];
+                S.bins[top - i] = 0;
+                sum += own[i];
             }
+            uint32_t above = group_scan<kWaves>(sum, S, turn++, &total);
+            if (above < need && above + sum >= need)
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) {
+                    if (above < need && above + own[i] >= need) {
+                        S.found[0] = top - i;
+                        S.found[1] = above;
+                        S.found[2] = own[i];
+                    }
+                    above += own[i];
+                }
             __syncthreads();
             const uint32_t in_bin = S.found[2];
             low += S.found[0] << shift;
@@ -362,7 +374,7 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
                 __syncthreads();
                 const uint32_t key = lane < in_bin ? S.last[lane] : 0;
                 uint32_t over = 0, same = 0;
-                for (uint32_t i = wave; i < in_bin; i += kSelectWaves) {
+                for (uint32_t i = wave; i < in_bin; i += kWaves) {
                     const uint32_t other = S.last[i];
                     over += other > key;
                     same += other == key;
@@ -389,7 +401,7 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         __syncthreads();
         uint32_t before = 0;
 #pragma unroll
-        for (uint32_t v = 0; v < kSelectWaves; ++v) before += v < wave ? S.part[turn & 1][v] : 0;
+        for (uint32_t v = 0; v < kWaves; ++v) before += v < wave ? S.part[turn & 1][v] : 0;
         ++turn;
         return before;
     };
@@ -447,11 +459,11 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
         holes += all & 0xffffu;
         movers += all >> 16;
     });
-    if (threadIdx.x == kSelectThreads - 1) S.found[0] = holes;
+    if (threadIdx.x == kThreads - 1) S.found[0] = holes;
     __threadfence_block();
     __syncthreads();  // the lists are whole, and nobody reads the slots that come free any more
     const uint32_t count = S.found[0];
-    for (uint32_t i = threadIdx.x; i < count; i += kSelectThreads) {
+    for (uint32_t i = threadIdx.x; i < count; i += kThreads) {
         const int32_t to = hole_list[i], from = mover_list[i];
         w_out[to] = w[from];
         pos_out[to] = pos[from];
@@ -459,7 +471,7 @@ __global__ __launch_bounds__(kSelectThreads) void endor_kv_select_kernel(EvictPa
     }
     if constexpr (kMove) {
         __syncthreads();
-        move_tokens(E.C, S.moves, count, kSelectThreads);
+        move_tokens(E.C, S.moves, count, kThreads);
     } else if (threadIdx.x == 0) {
         E.count[row] = count;
     }
@@ -490,15 +502,28 @@ __global__ __launch_bounds__(256) void endor_kv_shorten_kernel(EvictParams E) {
     E.lengths_out[b] = length < E.budget ? length : E.budget;
 }
 
+// The chunks are the fewest that hold the tokens in registers. Small workgroups have fewer waves to
+// wait for at each barrier, and two of them share a compute unit better than two large ones do; large
+// ones hold more tokens and work longer rows off sooner where there is one for each unit at most.
+// Measured with 512 | 1024 threads: 1 x 8 rows of 1025 tokens 7.2 | 8.9 us, 4 x 8 of 2049 8.9 | 9.6,
+// 1 x 8 of 4000 10.0 | 10.7, 64 x 8 of 1025 9.7 | 17.6, 8 x 72 of 3457 14.2 | 24.2, 64 x 8 of 16000
+// 40.5 | 46.4; but 13 x 16 of 6600 12.7 | 11.5 and 32 x 8 of 4097 13.3 | 13.4. With 256 threads all
+// but the shortest rows take longer: 4 x 8 of 2049 10.8, 8 x 72 of 3457 16.8.
 template <bool kMove>
 void launch_select(const EvictParams &E, hipStream_t s) {
-    constexpr int kChunk = 256 * kSelectWaves;
-    const auto kernel = E.most_len <= kChunk       ? endor_kv_select_kernel<1, kMove>
-                        : E.most_len <= 2 * kChunk ? endor_kv_select_kernel<2, kMove>
-                        : E.most_len <= 4 * kChunk ? endor_kv_select_kernel<4, kMove>
-                        : E.most_len <= 8 * kChunk ? endor_kv_select_kernel<8, kMove>
-                                                   : endor_kv_select_kernel<0, kMove>;
-    hipLaunchKernelGGL(kernel, dim3(E.C.kv_heads, E.C.batch), dim3(kSelectThreads), 0, s, E);
+    constexpr int kUnits = 256;
+    const int64_t rows = int64_t(E.C.batch) * E.C.kv_heads;
+    const bool small = E.most_len <= 4096 || (rows > kUnits && E.most_len <= 16384);
+    const int threads = small ? 512 : 1024, chunks = (E.most_len - 1) / (4 * threads) + 1;
+    const auto kernel = small ? chunks <= 1   ? endor_kv_select_kernel<512, 1, kMove>
+                                : chunks <= 2 ? endor_kv_select_kernel<512, 2, kMove>
+                                : chunks <= 4 ? endor_kv_select_kernel<512, 4, kMove>
+                                              : endor_kv_select_kernel<512, 8, kMove>
+                        : chunks <= 2 ? endor_kv_select_kernel<1024, 2, kMove>
+                        : chunks <= 4 ? endor_kv_select_kernel<1024, 4, kMove>
+                        : chunks <= 8 ? endor_kv_select_kernel<1024, 8, kMove>
+                                      : endor_kv_select_kernel<1024, 0, kMove>;
+    hipLaunchKernelGGL(kernel, dim3(E.C.kv_heads, E.C.batch), dim3(threads), 0, s, E);
 }
 
 // The most tokens of a sequence and head that move: as many as come free below the budget, or lie past it.

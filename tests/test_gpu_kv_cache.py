@@ -166,6 +166,19 @@ def test_evict_long(length):
         run_evict(lengths, lengths.copy(), w, pos, length // 2, 100, cache, k, v, table)
 
 
+@pytest.mark.parametrize("batch,heads,length", [(3, 72, 5000), (4, 72, 5000), (4, 72, 9001), (9, 30, 16384), (9, 30, 16385), (300, 1, 513)])
+def test_evict_many_rows(batch, heads, length):
+    """More rows than compute units, and fewer; with few moves and with many."""
+    print("evict rows", batch, heads, length, flush=True)
+    lengths = np.full(batch, length, np.int32)
+    lengths[0], lengths[-1] = length // 2, 7
+    cache, k, v, table, g = make(lengths, lengths, heads, 8, 64, seed=length)
+    for kind, budget in (("random", length - 20), ("ties", length // 3)):
+        w = statistics(g, batch, heads, cache.capacity, kind)
+        pos = np.broadcast_to(np.arange(cache.capacity, dtype=np.int32), w.shape).copy()
+        run_evict(lengths, lengths.copy(), w, pos, budget, budget // 4, cache, k, v, table)
+
+
 def test_evict_bounds_and_missing_pages():
     lengths = np.array([-3, 100, 2 ** 31 - 1, 90], np.int32)
     cache, k, v, table, g = make(lengths, [16, 100, 112, 96], 2, 64, 16, seed=8, gaps=True)
