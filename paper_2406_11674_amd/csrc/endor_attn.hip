@@ -2,22 +2,23 @@
 //     s_t = scale <q, k_t>,  out = sum_t exp(s_t - lse) v_t,  lse = log sum_t exp(s_t),
 // for all query heads that share a kv head in one pass over its keys and values.
 //
-// A wave takes 32 slots at a time.  Both products go to the matrix cores, with up to 16 query heads as the result's columns; one
-// head alone leaves 15 of 16 columns empty, which costs nothing: an instruction takes 16 clocks for 1 KB of keys that memory
-// brings in some 100.  S^T = K Q^T: a lane loads 16 bytes of the key of its row, straight into the operand's
-// registers.  Its result has a lane hold, for the query of its column, slots 4g + 0..3 and 16 + 4g + 0..3 (g: its quarter of the wave), which
-// is, with the slots in that order, the operand that O^T = V^T P^T wants: P never leaves the lane.  For V^T a lane loads, of those
-// 8 slots, 16 bytes each at dims 8n.. (n: its place in the quarter, so a quarter reads whole rows) and turns the 8 x 8
-// elements around in its registers (v_perm_b32): instruction j has dims 8m + j for rows m, and a lane ends up with 32 neighbouring
-// dims of its query.  Neither operand passes through LDS.
+// A wave takes 32 slots at a time. Both products go to the matrix cores, with up to 16 query heads as the result's
+// columns; one head alone leaves 15 of 16 columns empty, which costs nothing: an instruction takes 16 clocks for 1 KB
+// of keys that memory brings in some 100. S^T = K Q^T: a lane loads 16 bytes of the key of its row, straight into the
+// operand's registers. Its result has a lane hold, for the query of its column, slots 4g + 0..3 and 16 + 4g + 0..3 (g:
+// its quarter of the wave), which is, with the slots in that order, the operand that O^T = V^T P^T wants: P never
+// leaves the lane. For V^T a lane loads, of those 8 slots, 16 bytes each at dims 8n.. (n: its place in the quarter, so
+// a quarter reads whole rows) and turns the 8 x 8 elements around in its registers (v_perm_b32): instruction j has dims
+// 8m + j for rows m, and a lane ends up with 32 neighbouring dims of its query. Neither operand passes through LDS.
 //
 // Softmax: the running maximum m is raised only when a logit passes it by 4 (in powers of two), so that sums are
-// rescaled a few times in all; p = 2^(s - m + 11) then fills fp16's range (at most 2^15, and a p of 2^-35 of the largest still counts).
-// P enters the second product in two parts of the type, high and remainder, so that of 32 bits 2^-16 (bf16) or 2^-20 (fp16) is
-// lost and not 2^-9 or 2^-11: matrix instructions are not what bounds this.  m, the totals and all sums are fp32.
+// rescaled a few times in all; p = 2^(s - m + 11) then fills fp16's range (at most 2^15, and a p of 2^-35 of the
+// largest still counts). P enters the second product in two parts of the type, high and remainder, so that of 32 bits
+// 2^-16 (bf16) or 2^-20 (fp16) is lost and not 2^-9 or 2^-11: matrix instructions are not what bounds this. m, the
+// totals and all sums are fp32.
 //
-// Short sequences take one launch, a workgroup for a kv head's queries; longer ones are cut into parts, a workgroup each, which a second kernel joins; it
-// also adds the tokens' weights, from the logits that the first one left behind.
+// Short sequences take one launch, a workgroup for a kv head's queries; longer ones are cut into parts, a workgroup
+// each, which a second kernel joins; it also adds the tokens' weights, from the logits that the first one left behind.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -124,8 +125,9 @@ __device__ __forceinline__ float quarters_sum(float x) {
 
 // What a wave does with a tile, and what it has of one on its way.
 //
-// kDim: 64, 128 or 256; a narrower head is treated as the next of them: lanes past it read its first elements instead, which meet zeros in q or
-// end up in dims that nobody writes.  kSub: runs of 32 slots that a wave takes at a time, so that narrow heads keep as many bytes on their way.
+// kDim: 64, 128 or 256; a narrower head is treated as the next of them: lanes past it read its first elements instead,
+// which meet zeros in q or end up in dims that nobody writes. kSub: runs of 32 slots that a wave takes at a time, so
+// that narrow heads keep as many bytes on their way.
 template <int kDim, int kSub, bool kBf16>
 struct Tiles {
     static constexpr int kChunks = kDim / 32;          // instructions of a key's dot product
@@ -203,7 +205,8 @@ struct Tiles {
         }
         return p;
     }
-    // A page that is not there is read as page 0, which is, and its slots are not visible; so are those past the length.
+    // A page that is not there is read as page 0, which is, and its slots are not visible; so are those past the
+    // length.
     __device__ __forceinline__ int64_t row_of(uint32_t page, uint32_t t, uint32_t length) const {
         const uint32_t slot = (t < length ? t : length - 1) & ((1u << A.C.page_shift) - 1);
         return int64_t(page < A.C.num_pages ? page : 0) * A.C.page_stride + int64_t(slot) * A.C.slot_stride;
@@ -230,7 +233,8 @@ struct Tiles {
     static __device__ __forceinline__ uint64_t mask_of(const Unit &u, uint32_t t0) {
         return u.mask ? u.mask[(t0 < u.length ? t0 : u.length - 1) >> 6] : ~uint64_t(0);
     }
-    // The logits of the tile whose keys are loaded, in powers of two; `next` puts out the next tile's keys once these are used.
+    // The logits of the tile whose keys are loaded, in powers of two; `next` puts out the next tile's keys once these
+    // are used.
     template <class Next>
     __device__ __forceinline__ void logits_of(f32x4 (&s)[2 * kSub], Next next) {
 #pragma unroll
@@ -328,7 +332,8 @@ __device__ __forceinline__ float lse_of(float top, float total) { return total =
 // What is taken off a logit to make it a weight: all of them are -infinity where nothing is visible.
 __device__ __forceinline__ float offset_of(float top, float total) { return total == 0 ? 0.0f : top - kShift + log2f(total); }
 
-// Joins a workgroup's waves: every wave leaves its sums and its maximum in LDS, then a thread adds up single elements: f(query, dim, sum, maximum, total).
+// Joins a workgroup's waves: every wave leaves its sums and its maximum in LDS, then a thread adds up single elements:
+// f(query, dim, sum, maximum, total).
 template <class T, int kWaves, class F>
 __device__ __forceinline__ void join_waves(const AttnParams &A, const typename T::Unit &u, const T &tiles, float *s_join, F f) {
     constexpr int kDim = 16 * T::kPer * T::kParts;
@@ -359,8 +364,9 @@ __device__ __forceinline__ void join_waves(const AttnParams &A, const typename T
     }
 }
 
-// Short sequences: one workgroup for a unit, its waves take the tiles in turn and are joined in LDS.  The weights too are added here, from logits in LDS
-// (`pitch` floats a query; a group of more than 16 query heads goes by the other form, for two workgroups would add to the same weights).
+// Short sequences: one workgroup for a unit, its waves take the tiles in turn and are joined in LDS. The weights too
+// are added here, from logits in LDS (`pitch` floats a query; a group of more than 16 query heads goes by the other
+// form, for two workgroups would add to the same weights).
 template <int kDim, int kWaves, bool kBf16>
 __global__ __launch_bounds__(64 * kWaves) void endor_attn_kernel(AttnParams A, uint32_t pitch) {
     typedef Tiles<kDim, 1, kBf16> T;
@@ -385,8 +391,8 @@ __global__ __launch_bounds__(64 * kWaves) void endor_attn_kernel(AttnParams A, u
         tiles.load_query(u, b);
         uint64_t word = T::mask_of(u, t0);
         for (; t0 < u.length; t0 += kStep) {
-            // Loads come back in order, so what is wanted first goes out first: the pages of the tile after the next one, this tile's values; the
-            // next tile's keys follow when this one's have been used.
+            // Loads come back in order, so what is wanted first goes out first: the pages of the tile after the next
+            // one, this tile's values; the next tile's keys follow when this one's have been used.
             const typename T::Pages later = tiles.pages_of(u.table, t0 + 2 * kStep, most);
             tiles.load_values(u, t0, now);
             const uint64_t next_word = T::mask_of(u, t0 + kStep);
@@ -421,17 +427,20 @@ __global__ __launch_bounds__(64 * kWaves) void endor_attn_kernel(AttnParams A, u
     }
 }
 
-// Longer sequences are cut into parts, a workgroup each, of equal numbers of tiles; the waves take a part's tiles in turn, so that a workgroup reads
-// neighbouring slots, and workgroups of one sequence's heads, which lie side by side on its pages, follow each other.
+// Longer sequences are cut into parts, a workgroup each, of equal numbers of tiles; the waves take a part's tiles in
+// turn, so that a workgroup reads neighbouring slots, and workgroups of one sequence's heads, which lie side by side on
+// its pages, follow each other.
 //
-// How long parts are follows from the lengths, which only the device knows.  Sequences of like lengths are best cut into as many parts as make
-// one workgroup for every compute unit (64 sequences of 2048 slots, 8 heads of 64: 45 us uncut, 55 in two parts; 131072 slots of 8 heads of 128: 32 parts
-// 86, 128 parts 98); where lengths differ, several times as many let the short ones fill in behind the long (32 sequences of up to 4096: 54 us, 72 uncut).
-// (Workgroups or waves that stay and share out all tiles evenly were slower: on pages of their own, or by what finding their places costs.)
+// How long parts are follows from the lengths, which only the device knows. Sequences of like lengths are best cut into
+// as many parts as make one workgroup for every compute unit (64 sequences of 2048 slots, 8 heads of 64: 45 us uncut,
+// 55 in two parts; 131072 slots of 8 heads of 128: 32 parts 86, 128 parts 98); where lengths differ, several times as
+// many let the short ones fill in behind the long (32 sequences of up to 4096: 54 us, 72 uncut). (Workgroups or waves
+// that stay and share out all tiles evenly were slower: on pages of their own, or by what finding their places costs.)
 struct Part {
     uint32_t count, first, past;  // parts of the sequence; tiles of this one
 };
-// n / d for n up to 2^30 and d > 0: the float quotient is off by one at most where it is below 2^22, and a sequence has no more parts or tiles.
+// n / d for n up to 2^30 and d > 0: the float quotient is off by one at most where it is below 2^22, and a sequence has
+// no more parts or tiles.
 __device__ __forceinline__ uint32_t over(uint32_t n, uint32_t d) {
     uint32_t q = static_cast<uint32_t>(static_cast<float>(n) * __builtin_amdgcn_rcpf(static_cast<float>(d)));
     while (uint64_t(q) * d > n) --q;
@@ -486,8 +495,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kDi
     constexpr uint32_t kStep = kWaves * T::kSlots;
     extern __shared__ float s_join[];  // [wave][query][dim], [wave][query][2]
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // Workgroups go to the eight XCDs in turn: with the parts last, those that short sequences do not have are spread over all of them
-    // (with the parts first, four or eight of them, some XCDs had nothing but the ends of long sequences: 72 us for 58).
+    // Workgroups go to the eight XCDs in turn: with the parts last, those that short sequences do not have are spread
+    // over all of them (with the parts first, four or eight of them, some XCDs had nothing but the ends of long
+    // sequences: 72 us for 58).
     const uint32_t split = blockIdx.z, b = blockIdx.y, dim = A.C.dim;
     const uint32_t held = clamp_length(A.lengths[b], A.most_len), length = A.C.num_pages ? held : 0;
     const Part part = part_of(length, chunk_of(A, lane, held), T::kSlots, split);
@@ -503,8 +513,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kDi
         tiles.load_query(u, b);
         uint64_t word = T::mask_of(u, t0);
         for (; t0 < end; t0 += kStep) {
-            // Loads come back in order, so what is wanted first goes out first: the pages of the tile after the next one, this tile's values; the
-            // next tile's keys follow when this one's have been used.
+            // Loads come back in order, so what is wanted first goes out first: the pages of the tile after the next
+            // one, this tile's values; the next tile's keys follow when this one's have been used.
             const typename T::Pages later = tiles.pages_of(u.table, t0 + 2 * kStep, end);
             tiles.load_values(u, t0, now);
             const uint64_t next_word = T::mask_of(u, t0 + kStep);
@@ -563,8 +573,9 @@ __device__ __forceinline__ float2 joined(const float2 *ml, uint32_t parts, uint3
 constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
 constexpr int kSlots = 2048;  // slots of a workgroup that adds weights
 
-// After the parts: the first `joins` workgroups join those of `heads` query heads each, where there are several, kJoinWaves / heads waves a head,
-// a lane four dims of every so many parts.  The others add the weights of kSlots slots of a kv head.
+// After the parts: the first `joins` workgroups join those of `heads` query heads each, where there are several,
+// kJoinWaves / heads waves a head, a lane four dims of every so many parts. The others add the weights of kSlots slots
+// of a kv head.
 template <bool kBf16>
 __global__ __launch_bounds__(kJoinThreads) void endor_attn_join_kernel(AttnParams A, uint32_t joins, uint32_t heads, uint32_t pieces) {
     __shared__ f32x4 s_sum[kJoinThreads];

@@ -32,15 +32,17 @@ inline Plan make_plan(int batch, int kv_heads, int q_heads, int dim, int32_t max
     p.units = static_cast<uint32_t>(kv_heads) * p.qtiles;
     p.row = static_cast<int32_t>((int64_t(max_len) + 63) / 64 * 64);
     const int64_t units = int64_t(batch) * p.units;
-    // One launch where a compute unit reads its share in about the time of the second one (1024 slots of one head of 64, or 512 of 128: 8.6 us in one
-    // launch, 8.8 in two; 1024 of 128 17.8 and 10.8), or where the units fill half of the chip by themselves (256 of 1000 slots: 24.7 and 29.5).
+    // One launch where a compute unit reads its share in about the time of the second one (1024 slots of one head of
+    // 64, or 512 of 128: 8.6 us in one launch, 8.8 in two; 1024 of 128 17.8 and 10.8), or where the units fill half of
+    // the chip by themselves (256 of 1000 slots: 24.7 and 29.5).
     if (max_len <= 1024 && units <= 512 && (int64_t(max_len) * dim <= 65536 || units >= 128) && (p.qtiles == 1 || !with_weights)) return p;
     // Where four waves to a compute unit would have less than two tiles each, two of them.
     p.waves = int64_t(max_len) * units >= 256 * 256 ? 4 : 2;
     p.least = 64 * p.waves;
     p.even = units < 256 ? static_cast<int32_t>(256 / units) : 1;
-    // Workgroups that have no part hold up others, and a part costs what its start and its join take: some six workgroups for every compute
-    // unit (of widest heads one, for the registers of one fill it), and four tiles of 64 slots or more for two waves.
+    // Workgroups that have no part hold up others, and a part costs what its start and its join take: some six
+    // workgroups for every compute unit (of widest heads one, for the registers of one fill it), and four tiles of 64
+    // slots or more for two waves.
     const int64_t groups = dim <= 128 ? 1536 : 256;
     int64_t chunk = ((int64_t(max_len) * units + groups - 1) / groups + 63) / 64 * 64;
     if (chunk > p.row) chunk = p.row;

@@ -36,8 +36,8 @@ struct AppendParams {
     int32_t tokens, capacity;
 };
 
-// Tokens first to first + count of heads head0 to head0 + heads of a sequence.  Threads: x the 16-byte units of a head's key or value, y the
-// keys and then the values of the heads and on to the next token, four of them on their way.
+// Tokens first to first + count of heads head0 to head0 + heads of a sequence. Threads: x the 16-byte units of a head's
+// key or value, y the keys and then the values of the heads and on to the next token, four of them on their way.
 __device__ __forceinline__ void store_tokens(const AppendParams &A, uint32_t b, uint32_t head0, uint32_t heads, uint32_t length, uint32_t seen,
                                              uint32_t first, uint32_t count) {
     typedef u32x4 u32x4_any __attribute__((aligned(2)));
@@ -100,7 +100,8 @@ __global__ __launch_bounds__(1024) void endor_kv_append_kernel(AppendParams A) {
 
 constexpr uint32_t kTokensEach = 8;
 
-// Prompts: kTokensEach tokens of a few heads a workgroup, so that a thread has four units of a head's; a second launch advances the lengths.
+// Prompts: kTokensEach tokens of a few heads a workgroup, so that a thread has four units of a head's; a second launch
+// advances the lengths.
 __global__ __launch_bounds__(256) void endor_kv_append_many_kernel(AppendParams A, uint32_t heads_each) {
     const uint32_t b = blockIdx.z, first = blockIdx.x * kTokensEach, head0 = blockIdx.y * heads_each;
     const uint32_t length = clamp_length(A.lengths[b], A.capacity), stored = stored_of(A, b, length), heads = A.C.kv_heads;
@@ -131,7 +132,8 @@ struct EvictParams {
     int32_t budget, recent, most_len, capacity, most;
 };
 
-// Weights as unsigned numbers in the same order: NaN 1, below all, -0 with +0; what must stay is above all.  0 is no token.
+// Weights as unsigned numbers in the same order: NaN 1, below all, -0 with +0; what must stay is above all. 0 is no
+// token.
 __device__ __forceinline__ uint32_t key_of(float w, int32_t position, int64_t newest) {
     if (position >= newest) return 0xffffffffu;
     if (w != w) return 1;
@@ -165,7 +167,8 @@ struct SelectShared {
     Move moves[kFewMoves];
 };
 
-// Exclusive prefix over the workgroup, and the total.  `turn` changes from one call to the next, so that one barrier does.
+// Exclusive prefix over the workgroup, and the total. `turn` changes from one call to the next, so that one barrier
+// does.
 template <uint32_t kWaves>
 __device__ __forceinline__ uint32_t group_scan(uint32_t x, SelectShared &S, uint32_t turn, uint32_t *total) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -203,15 +206,16 @@ __device__ __forceinline__ void move_tokens(const Cache &C, const Move *moves, u
     }
 }
 
-// One workgroup per sequence and kv head finds the key of the last token that stays, then the slots that come free below the budget and the
-// kept ones past it, in order.
+// One workgroup per sequence and kv head finds the key of the last token that stays, then the slots that come free
+// below the budget and the kept ones past it, in order.
 //
-// The keys are looked at 11 bits at a time from the highest bit in which they differ: a histogram in LDS, and a scan of it from
-// the top, until a wave can hold what is left and count for each key those above it.  (Weights of one row share most of their leading
-// bits: a fixed first digit would have nearly all keys in a few bins, where LDS adds them one after the other.)  A wave has a contiguous piece of the slots, 256 of them at a
-// time, four to a lane: loads are whole lines, and ranks in the order of slots need wave scans only.  kChunks: such chunks of a wave that it
-// keeps as keys in registers; 0: the keys are formed anew in every pass, for rows past 32768 slots.
-// kMove: the moves are few and done here.
+// The keys are looked at 11 bits at a time from the highest bit in which they differ: a histogram in LDS, and a scan of
+// it from the top, until a wave can hold what is left and count for each key those above it. (Weights of one row share
+// most of their leading bits: a fixed first digit would have nearly all keys in a few bins, where LDS adds them one
+// after the other.) A wave has a contiguous piece of the slots, 256 of them at a time, four to a lane: loads are whole
+// lines, and ranks in the order of slots need wave scans only. kChunks: such chunks of a wave that it keeps as keys in
+// registers; 0: the keys are formed anew in every pass, for rows past 32768 slots. kMove: the moves are few and done
+// here.
 template <int kThreads, int kChunks, bool kMove>
 __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E) {
     constexpr uint32_t kWaves = kThreads / 64;
@@ -394,7 +398,8 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
         }
     }
 
-    // Which stay: above, or equal and among the first.  Of the waves before this one: equal keys, then slots that come free and tokens that move.
+    // Which stay: above, or equal and among the first. Of the waves before this one: equal keys, then slots that come
+    // free and tokens that move.
     auto waves_before = [&](uint32_t x) {
         const uint32_t sum = wave_sum(x);
         if (lane == 0) S.part[turn & 1][wave] = sum;

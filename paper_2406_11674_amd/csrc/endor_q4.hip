@@ -1,11 +1,12 @@
 // Products with 4-bit weights that carry a scale, and if wanted a zero point, per row and group of columns.
 //
-// PACKED FORM.  Rows go in tiles of 16, columns in blocks of 128, both padded with codes and scales of zero, so that no
-// kernel has an edge in W.  Codes: [tile][block][lane 0..63][16 bytes]; lane l has row l & 15 of the tile, and its 32-bit word j the
-// columns 32 j + 8 (l >> 4) + 0..7 of the block, the even ones in the lower half and the odd ones in the upper, 4 bits each.  Then the scales, fp16, for a tile and a block (or a
-// group that holds blocks): [4 quarters][groups of the block][4 rows], as the lanes of a product's result want them; then, if there
-// are any, the zeros, bytes [16 rows][groups of the block], as the lanes of its operand do.  A block and a group that holds several blocks end
-// at the same column.
+// PACKED FORM. Rows go in tiles of 16, columns in blocks of 128, both padded with codes and scales of zero, so that no
+// kernel has an edge in W. Codes: [tile][block][lane 0..63][16 bytes]; lane l has row l & 15 of the tile, and its
+// 32-bit word j the columns 32 j + 8 (l >> 4) + 0..7 of the block, the even ones in the lower half and the odd ones in
+// the upper, 4 bits each. Then the scales, fp16, for a tile and a block (or a group that holds blocks): [4
+// quarters][groups of the block][4 rows], as the lanes of a product's result want them; then, if there are any, the
+// zeros, bytes [16 rows][groups of the block], as the lanes of its operand do. A block and a group that holds several
+// blocks end at the same column.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -61,8 +62,8 @@ struct PackParams {
     int64_t rows, cols, group, groups, tiles, blocks, padded_groups;
 };
 
-// Eight columns' codes as a checkpoint has them, column c in bits 4c, with the even columns in the lower half: pairs of columns lie 16 bits
-// apart then, where packed 16-bit arithmetic takes them.
+// Eight columns' codes as a checkpoint has them, column c in bits 4c, with the even columns in the lower half: pairs of
+// columns lie 16 bits apart then, where packed 16-bit arithmetic takes them.
 __device__ __forceinline__ uint32_t even_below_odd(uint32_t x) {
     auto squeeze = [](uint32_t v) {  // the low halves of four bytes side by side
         v &= 0x0f0f0f0fu;
@@ -108,7 +109,8 @@ __global__ __launch_bounds__(256) void endor_q4_pack_kernel(PackParams P) {
     }
 }
 
-// One wave per row and group.  The scale is rounded to fp16 before the codes are taken, so that they are the nearest to what they stand for.
+// One wave per row and group. The scale is rounded to fp16 before the codes are taken, so that they are the nearest to
+// what they stand for.
 __global__ __launch_bounds__(64) void endor_q4_quantize_kernel(const _Float16 *dense, int64_t first, int64_t cols, int64_t group, int64_t groups,
                                                                uint8_t *codes, _Float16 *scales, uint8_t *zeros) {
     const int64_t i = first + blockIdx.x, row = i / groups, g = i % groups, from = g * group;
@@ -231,7 +233,8 @@ __device__ __forceinline__ f32x4 product(u32x4 a, u32x4 b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// What a wave has of W on its way: a block of 128 columns of kTiles row tiles, with the scales and zeros of its groups (kParts of them).
+// What a wave has of W on its way: a block of 128 columns of kTiles row tiles, with the scales and zeros of its groups
+// (kParts of them).
 template <int kTiles, int kParts, bool kZeros>
 struct Block {
     u32x4 codes[kTiles];
@@ -270,7 +273,8 @@ __device__ __forceinline__ void add_block(f32x4 (&total)[kTiles], const Block<kT
         }
 }
 
-// The waves' sums are added in their order; a lane has rows 4g + 0..3 of every tile for the right-hand side of its column.
+// The waves' sums are added in their order; a lane has rows 4g + 0..3 of every tile for the right-hand side of its
+// column.
 template <int kTiles>
 __device__ __forceinline__ void join_waves(const Q4Params &Q, float *s_part, uint32_t tile0, const f32x4 (&total)[kTiles]) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, n = lane & 15, g = lane >> 4;
@@ -299,8 +303,8 @@ __device__ __forceinline__ u32x4 columns_of(const uint16_t *x, int64_t c, int64_
     return v;
 }
 
-// Few right-hand sides: all of x lies in LDS, in the order of the operands, [block][32 columns][quarter][right-hand side][8 columns].
-// A workgroup has one row tile, its waves take the blocks in turn, kDepth of them on their way.
+// Few right-hand sides: all of x lies in LDS, in the order of the operands, [block][32 columns][quarter][right-hand
+// side][8 columns]. A workgroup has one row tile, its waves take the blocks in turn, kDepth of them on their way.
 template <int kDepth, int kParts, bool kZeros, bool kBf16>
 __global__ __launch_bounds__(1024) void endor_q4_gemv_kernel(Q4Params Q) {
     extern __shared__ u32x4 s_x[];

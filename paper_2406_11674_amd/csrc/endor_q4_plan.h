@@ -20,8 +20,9 @@ inline size_t x_bytes(uint32_t blocks, uint32_t nb) { return size_t(blocks) * 25
 
 inline Plan make_plan(uint32_t tiles, uint32_t blocks, uint32_t nb) {
     Plan p{};
-    // Few row tiles leave compute units empty: the columns are split over several workgroups, where that saves more than the second
-    // launch that adds them up costs (2.5 us).  A block takes a workgroup some 0.04 us with x in LDS, 0.1 otherwise.
+    // Few row tiles leave compute units empty: the columns are split over several workgroups, where that saves more
+    // than the second launch that adds them up costs (2.5 us). A block takes a workgroup some 0.04 us with x in LDS,
+    // 0.1 otherwise.
     p.splits = 1;
     if (tiles <= 128) {
         uint32_t most = 256 / tiles;
