@@ -158,9 +158,10 @@ struct Q4Params {
 struct Pairs {  // fp16
     f16x2 near, far;
     uint32_t mask, one;  // kept in registers, so that a pair takes one instruction
-    __device__ __forceinline__ explicit Pairs(float z) : mask(0x000f000fu), one(0x64006400u) {
-        near = f16x2{static_cast<_Float16>(-1024.0f - z), static_cast<_Float16>(-1024.0f - z)};
-        far = f16x2{static_cast<_Float16>(-64.0f - z), static_cast<_Float16>(-64.0f - z)};
+    // z: the zero in both halves; -(1024 + z) and -(64 + z), whose last bits stand for 1 and for a sixteenth
+    __device__ __forceinline__ explicit Pairs(uint32_t z) : mask(0x000f000fu), one(0x64006400u) {
+        near = __builtin_bit_cast(f16x2, z | 0xe400e400u);
+        far = __builtin_bit_cast(f16x2, z << 4 | 0xd400d400u);
         asm("" : "+s"(mask));
         asm("" : "+v"(one));
     }
@@ -181,7 +182,7 @@ template <bool kZeros>
 struct Operand<false, kZeros> {
     static constexpr float kUnit = 1.0f;
     Pairs pairs;
-    __device__ __forceinline__ explicit Operand(float z) : pairs(z) {}
+    __device__ __forceinline__ explicit Operand(uint32_t z) : pairs(z) {}
     __device__ __forceinline__ u32x4 of(uint32_t w) const {
         f16x2 p[4];
         pairs.get(w, p);
@@ -192,7 +193,7 @@ template <>
 struct Operand<true, true> {
     static constexpr float kUnit = 1.0f;
     Pairs pairs;
-    __device__ __forceinline__ explicit Operand(float z) : pairs(z) {}
+    __device__ __forceinline__ explicit Operand(uint32_t z) : pairs(z) {}
     __device__ __forceinline__ u32x4 of(uint32_t w) const {
         f16x2 p[4];
         pairs.get(w, p);
@@ -208,7 +209,7 @@ struct Operand<true, true> {
 template <>
 struct Operand<true, false> {  // code - 8, of which the instruction makes a sixteenth
     static constexpr float kUnit = 16.0f;
-    __device__ __forceinline__ explicit Operand(float) {}
+    __device__ __forceinline__ explicit Operand(uint32_t) {}
     __device__ __forceinline__ u32x4 of(uint32_t w) const {
         const uint32_t low = w ^ 0x88888888u, high = low >> 4;
         auto pair = [&](uint32_t v, int a) {
@@ -264,7 +265,7 @@ __device__ __forceinline__ void add_block(f32x4 (&total)[kTiles], const Block<kT
     for (int r = 0; r < kTiles; ++r)
 #pragma unroll
         for (int p = 0; p < kParts; ++p) {
-            const Operand<kBf16, kZeros> operand(kZeros ? static_cast<float>(B.zeros[r] >> (8 * p) & 0xffu) : 8.0f);
+            const Operand<kBf16, kZeros> operand(kZeros ? __builtin_amdgcn_perm(0, B.zeros[r], 0x0c000c00u | p << 16 | p) : 0x00080008u);
             f32x4 sum = {0, 0, 0, 0};
 #pragma unroll
             for (int j = 4 / kParts * p; j < 4 / kParts * (p + 1); ++j) sum = product<kBf16>(operand.of(B.codes[r][j]), x[j], sum);
@@ -381,15 +382,28 @@ __global__ __launch_bounds__(256) void endor_q4_join_kernel(const float *partial
 }
 
 template <int kParts, bool kZeros, bool kBf16>
+void (*gemm_kernel(const Plan &p))(Q4Params) {
+    if (p.tiles == 0) {
+        if constexpr (kParts < 4)  // with a group of 32 one block is on its way
+            if (p.depth == 2) return endor_q4_gemv_kernel<2, kParts, kZeros, kBf16>;
+        return endor_q4_gemv_kernel<1, kParts, kZeros, kBf16>;
+    }
+    if constexpr (kParts < 4) {  // and there are at most five row tiles
+        if (p.tiles == 7) return endor_q4_gemm_kernel<7, kParts, kZeros, kBf16>;
+        if (p.tiles == 6) return endor_q4_gemm_kernel<6, kParts, kZeros, kBf16>;
+    }
+    return p.tiles == 5   ? endor_q4_gemm_kernel<5, kParts, kZeros, kBf16>
+           : p.tiles == 4 ? endor_q4_gemm_kernel<4, kParts, kZeros, kBf16>
+           : p.tiles == 3 ? endor_q4_gemm_kernel<3, kParts, kZeros, kBf16>
+           : p.tiles == 2 ? endor_q4_gemm_kernel<2, kParts, kZeros, kBf16>
+                          : endor_q4_gemm_kernel<1, kParts, kZeros, kBf16>;
+}
+template <int kParts, bool kZeros, bool kBf16>
 void launch(const Q4Params &Q, const Plan &p, hipStream_t s) {
     const uint32_t tiles = p.tiles ? p.tiles : 1;
     size_t lds = size_t(p.waves) * Q.nb * tiles * 16 * sizeof(float);
     if (!p.tiles && lds < endor_q4_plan::x_bytes(p.per_split, Q.nb)) lds = endor_q4_plan::x_bytes(p.per_split, Q.nb);
-    const auto kernel = p.tiles == 4   ? endor_q4_gemm_kernel<4, kParts, kZeros, kBf16>
-                        : p.tiles == 2 ? endor_q4_gemm_kernel<2, kParts, kZeros, kBf16>
-                        : p.tiles == 1 ? endor_q4_gemm_kernel<1, kParts, kZeros, kBf16>
-                        : p.depth == 2 ? endor_q4_gemv_kernel<2, kParts, kZeros, kBf16>
-                                       : endor_q4_gemv_kernel<1, kParts, kZeros, kBf16>;
+    const auto kernel = gemm_kernel<kParts, kZeros, kBf16>(p);
     hipLaunchKernelGGL(kernel, dim3((Q.tiles + tiles - 1) / tiles, p.splits), dim3(64 * p.waves), lds, s, Q);
 }
 template <int kParts>
@@ -423,7 +437,7 @@ extern "C" size_t endor_q4_bytes(int64_t rows, int64_t cols, int group, int with
 extern "C" size_t endor_q4_scratch_bytes(int64_t rows, int64_t cols, int group, int nb) {
     if (!sizes_ok(rows, cols, group) || nb < 1 || nb > ENDOR_GEMM_MAX_BATCH || rows == 0 || cols == 0) return 0;
     const Layout l = layout_of(rows, cols, group, false);
-    const Plan p = make_plan(static_cast<uint32_t>(l.tiles), static_cast<uint32_t>(l.blocks), static_cast<uint32_t>(nb));
+    const Plan p = make_plan(static_cast<uint32_t>(l.tiles), static_cast<uint32_t>(l.blocks), static_cast<uint32_t>(nb), group);
     return p.splits > 1 ? (size_t(p.splits) * nb * rows * sizeof(float) + 255) & ~size_t(255) : 0;
 }
 
@@ -507,7 +521,7 @@ extern "C" endor_status endor_q4_gemm(int64_t rows, int64_t cols, int group, int
     Q.groups = static_cast<uint32_t>(l.groups);
     Q.per_group_shift = group > 128 ? static_cast<uint32_t>(__builtin_ctz(static_cast<unsigned>(group))) - 7 : 0;
     Q.nb = static_cast<uint32_t>(nb);
-    const Plan p = make_plan(Q.tiles, Q.blocks, Q.nb);
+    const Plan p = make_plan(Q.tiles, Q.blocks, Q.nb, group);
     if (p.splits > 1) {
         if (!aligned(d_scratch, 256)) return ENDOR_ERR_INVALID_ARG;
         if (scratch_bytes < endor_q4_scratch_bytes(rows, cols, group, nb)) return ENDOR_ERR_BUFFER_TOO_SMALL;

@@ -52,18 +52,18 @@ static const char *check_attn(int batch, int kv, int group, int dim, int32_t mos
     return nullptr;
 }
 
-static const char *check_q4(uint32_t tiles, uint32_t blocks, uint32_t nb) {
+static const char *check_q4(uint32_t tiles, uint32_t blocks, uint32_t nb, int group) {
     using namespace endor_q4_plan;
-    const Plan p = make_plan(tiles, blocks, nb);
+    const Plan p = make_plan(tiles, blocks, nb, group);
     if (p.splits < 1 || p.splits > 65535 || uint64_t(p.splits) * p.per_split < blocks) return "columns left out";
     if (uint64_t(p.splits - 1) * p.per_split >= blocks) return "a part without columns";
     if (p.tiles == 0) {
         if (p.waves != 4 && p.waves != 8 && p.waves != 16) return "waves";
-        if (p.depth != 1 && p.depth != 2) return "depth";
+        if (p.depth != 1 && (p.depth != 2 || group == 32)) return "depth";
         if (x_bytes(p.per_split, nb) > (128u << 10)) return "x takes more LDS than it may";
         if (size_t(p.waves) * nb * 64 > (160u << 10)) return "sums take more LDS than there is";
     } else {
-        if (p.tiles != 1 && p.tiles != 2 && p.tiles != 4) return "tiles";
+        if (p.tiles < 1 || p.tiles > (group == 32 ? 5 : 7)) return "tiles";
         if (p.waves != 4 && p.waves != 8) return "waves";
         if (size_t(p.waves) * nb * p.tiles * 64 > (160u << 10)) return "sums take more LDS than there is";
     }
@@ -81,7 +81,8 @@ int main() {
     }
     for (int i = 0; i < 200000; ++i) {
         const uint32_t tiles = static_cast<uint32_t>(size(20)), blocks = static_cast<uint32_t>(size(18)), nb = 1 + rnd() % 16;
-        if (const char *what = check_q4(tiles, blocks, nb)) {
+        const int group = 32 << rnd() % 4;
+        if (const char *what = check_q4(tiles, blocks, nb, group)) {
             std::printf("4-bit product of %u row tiles and %u blocks, %u right-hand sides: %s\n", tiles, blocks, nb, what);
             return 1;
         }

@@ -72,6 +72,17 @@ def test_larger(shape):
         check(m, w, torch.from_numpy(g.standard_normal((nb, cols), dtype=np.float32)).to(TYPES[dtype]))
 
 
+@pytest.mark.parametrize("zeros", [False, True], ids=["sym", "zeros"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("rows", [4100, 8200, 11111, 16001, 20011, 24001, 28001, 32005, 57400])
+def test_row_tiles(rows, group, zeros):
+    """One row tile to seven of them for a workgroup."""
+    print("q4 rows", rows, group, zeros, flush=True)
+    m, w, g = make(rows, 900, group, zeros, seed=rows)
+    for nb, dtype in ((2, "f16"), (13, "bf16"), (16, "f16")):
+        check(m, w, torch.from_numpy(g.standard_normal((nb, 900), dtype=np.float32)).to(TYPES[dtype]))
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_strides_and_alignment(dtype):
     """Rows of x at every 2-byte alignment, with NaN between and behind them, and y between guards."""
