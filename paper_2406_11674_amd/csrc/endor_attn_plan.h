@@ -39,11 +39,26 @@ inline Plan make_plan(int batch, int kv_heads, int q_heads, int dim, int32_t max
     // Where four waves to a compute unit would have less than two tiles each, two of them.
     p.waves = int64_t(max_len) * units >= 256 * 256 ? 4 : 2;
     p.least = 64 * p.waves;
-    p.even = units < 256 ? static_cast<int32_t>(256 / units) : 1;
-    // Workgroups that have no part hold up others, and a part costs what its start and its join take: some six
+    // Sequences of like lengths are cut where that fills the chip more evenly than it costs: the compute units with the
+    // most workgroups take `turns` of them, each the time that 40 KB/us take for its slots and some 1.5 us to begin and
+    // to join. (19 sequences of 4001 slots, 8 heads of 64: uncut 43.7 us, in three 34.8, in five 34.1; 8 of 2048, 72
+    // heads of 128: 118, in two 111; 64 of 2048, 8 heads of 64: 49.5, in two 54; one of 131072, 8 heads of 128: in 32
+    // 87, in 27 92, in 128 98.)
+    constexpr int64_t kMostGroups = 1536;
+    const double uncut = static_cast<double>(max_len) * dim * 4 / 40e3;
+    double least_time = 0;
+    p.even = 1;
+    for (int64_t turns = (units + 255) / 256; turns * 256 <= kMostGroups; ++turns) {
+        const int64_t parts = 256 * turns / units;
+        const double time = static_cast<double>(turns) * (uncut / static_cast<double>(parts) + 1.5);
+        if (least_time > 0 && time >= least_time) continue;
+        least_time = time;
+        p.even = static_cast<int32_t>(parts);
+    }
+    // Others: workgroups that have no part hold up others, and a part costs what its start and its join take: some six
     // workgroups for every compute unit (of widest heads one, for the registers of one fill it), and four tiles of 64
     // slots or more for two waves.
-    const int64_t groups = dim <= 128 ? 1536 : 256;
+    const int64_t groups = dim <= 128 ? kMostGroups : 256;
     int64_t chunk = ((int64_t(max_len) * units + groups - 1) / groups + 63) / 64 * 64;
     if (chunk > p.row) chunk = p.row;
     if (chunk < 2 * p.least) chunk = 2 * p.least;
@@ -56,9 +71,9 @@ inline Plan make_plan(int batch, int kv_heads, int q_heads, int dim, int32_t max
     if (p.splits < 1) p.splits = 1;
     p.heads = p.splits <= 16 ? 8 : 1;
     // Scratch is what the largest plan up to max_len takes, so that scratch for a bound serves every lower one too.
-    const int64_t ceiling = (groups + units - 1) / units;
+    const int64_t ceiling = (kMostGroups + units - 1) / units;
     int64_t parts = (int64_t(max_len) + 127) / 128;
-    if (parts > (ceiling > p.even ? ceiling : p.even)) parts = ceiling > p.even ? ceiling : p.even;
+    if (parts > ceiling) parts = ceiling;
     const size_t rows = size_t(batch) * q_heads;
     p.partial = parts > 1 ? round256(rows * parts * dim * 4) : 0;
     p.ml = round256(rows * parts * 8);
