@@ -73,7 +73,8 @@ __device__ __forceinline__ uint32_t even_below_odd(uint32_t x) {
     return squeeze(x) | squeeze(x >> 4) << 16;
 }
 
-// A thread makes a lane's 16 bytes of a block; the first ones of a workgroup the scales and zeros.
+// A thread makes a lane's 16 bytes of a block; the first ones of a workgroup the scales and zeros. Bound by memory: 28672 x
+// 8192, 242 MB read and written in 67 us.
 __global__ __launch_bounds__(256) void endor_q4_pack_kernel(PackParams P) {
     const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, units = P.tiles * P.blocks * 64;
     if (i < units) {
@@ -305,7 +306,9 @@ __device__ __forceinline__ u32x4 columns_of(const uint16_t *x, int64_t c, int64_
 }
 
 // Few right-hand sides: all of x lies in LDS, in the order of the operands, [block][32 columns][quarter][right-hand
-// side][8 columns]. A workgroup has one row tile, its waves take the blocks in turn, kDepth of them on their way.
+// side][8 columns]. A workgroup has one row tile, its waves take the blocks in turn, kDepth of them on their way. Bound by
+// memory: 8192 x 28672 with groups of 128 and one right-hand side 22 us, 121 MB at 5.5 TB/s; small ones by what comes
+// before the first product, 1024 x 8192 5.6 us.
 template <int kDepth, int kParts, bool kZeros, bool kBf16>
 __global__ __launch_bounds__(1024) void endor_q4_gemv_kernel(Q4Params Q) {
     extern __shared__ u32x4 s_x[];
@@ -338,7 +341,10 @@ __global__ __launch_bounds__(1024) void endor_q4_gemv_kernel(Q4Params Q) {
     join_waves<1>(Q, reinterpret_cast<float *>(s_x), blockIdx.x, total);
 }
 
-// More right-hand sides: x comes from the caches, once for kTiles row tiles.
+// More right-hand sides: x comes from the caches, once for kTiles row tiles. Bound by memory and by the vector ALUs
+// together, which make numbers of codes (9 instructions for 8 codes of fp16, 13 or 21 of bf16) and scale the sums: 28672 x
+// 8192 with 16 right-hand sides, groups of 64 and zeros 25.2 us, 131 MB at 5.2 TB/s; bf16 with groups of 32 42. A second
+// block on its way takes as long or longer (8192 x 8192 12.5 us, 13.8 with two), so it is not latency that it waits for.
 template <int kTiles, int kParts, bool kZeros, bool kBf16>
 __global__ __launch_bounds__(512) void endor_q4_gemm_kernel(Q4Params Q) {
     extern __shared__ float s_part[];
@@ -373,6 +379,7 @@ __global__ __launch_bounds__(512) void endor_q4_gemm_kernel(Q4Params Q) {
     join_waves<kTiles>(Q, s_part, tile0, total);
 }
 
+// Adds the parts of the columns, in their order: a launch and its trip to memory, 2.5 us.
 __global__ __launch_bounds__(256) void endor_q4_join_kernel(const float *partial, float *y, int64_t count, uint32_t splits) {
     const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
     if (i >= count) return;

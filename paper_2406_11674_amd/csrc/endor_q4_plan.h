@@ -22,7 +22,7 @@ inline Plan make_plan(uint32_t tiles, uint32_t blocks, uint32_t nb, int group) {
     Plan p{};
     // Few row tiles leave compute units empty: the columns are split over several workgroups, where that saves more
     // than the second launch that adds them up costs (2.5 us). A block takes a workgroup some 0.04 us with x in LDS,
-    // 0.1 otherwise.
+    // 0.1 otherwise. (1024 x 28672 with two right-hand sides 11.5 us, split 8.3; 2048 x 20000 with four 18 and 10.)
     p.splits = 1;
     if (tiles <= 128) {
         uint32_t most = 256 / tiles;
