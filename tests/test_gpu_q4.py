@@ -182,6 +182,33 @@ def test_quantize(zeros):
                 assert abs(float(s[i, gi]) - want) <= want * 2.0 ** -10 + 2.0 ** -24
 
 
+@pytest.mark.parametrize("zeros", [False, True], ids=["sym", "zeros"])
+@pytest.mark.parametrize("group", [32, 64, 128, 256, 512, 1024, 32768])
+def test_quantize_every_group(group, zeros):
+    """Codes, scales and zero points exactly: the definition takes one fp32 step after the other."""
+    g = np.random.default_rng(group)
+    for rows, cols in ((1, 1), (3, 33), (67, 1031), (5, 2048), (2, 70001)):
+        print("quantize", rows, cols, flush=True)
+        dense = (g.standard_normal((rows, cols)) * 0.02).astype(np.float16)
+        dense[0, :min(cols, group)] = 0
+        codes, scales, points = endor.q4_quantize(torch.from_numpy(dense).cuda(), group, zeros)
+        groups = -(-cols // group)
+        x = np.zeros((rows, groups * group), np.float32)
+        x[:, :cols] = dense
+        x = x.reshape(rows, groups, group)
+        lo, hi = np.minimum(x.min(2), 0), np.maximum(x.max(2), 0)
+        s = ((hi - lo) / np.float32(15) if zeros else np.maximum(hi, -lo) / np.float32(7)).astype(np.float16)
+        with np.errstate(divide="ignore"):
+            inverse = np.where(s > 0, np.float32(1) / s.astype(np.float32), np.float32(0)).astype(np.float32)
+        z = np.clip(np.rint(-lo * inverse), 0, 15) if zeros else np.full_like(inverse, 8)
+        c = np.clip(np.rint(x * inverse[..., None]) + z[..., None], 0, 15).astype(np.uint8).reshape(rows, -1)
+        c[:, cols:] = 0
+        both = c[:, :(cols + 1) // 2 * 2]
+        assert np.array_equal(scales.cpu().numpy(), s)  # of the two zeros either
+        assert points is None or np.array_equal(points.cpu().numpy(), z.astype(np.uint8))
+        assert np.array_equal(codes.cpu().numpy(), both[:, 0::2] | both[:, 1::2] << 4)
+
+
 def test_refusals():
     m, w, g = make(16, 128, 64, True)
     x = torch.zeros((2, 128), dtype=torch.float16, device="cuda")
