@@ -179,6 +179,31 @@ def test_evict_many_rows(batch, heads, length):
         run_evict(lengths, lengths.copy(), w, pos, budget, budget // 4, cache, k, v, table)
 
 
+@pytest.mark.parametrize("budget", [360, 150])
+def test_offsets_past_32_bits(budget):
+    """Pages whose elements lie past 2^32 elements from the start of the pool: appended to, then evicted from."""
+    page, dim, kv, length = 128, 64, 1, 371
+    far = (1 << 32) // 4 + 64  # elements between pages: page 5 begins past 2^32
+    buf = torch.empty(5 * far + 2 * page * dim, dtype=torch.float16, device="cuda")
+    kd, vd = (torch.as_strided(buf, (6, kv, page, dim), (far, page * dim, dim, 1), at) for at in (0, page * dim))
+    g = np.random.default_rng(17)
+    k, v = (g.integers(-2 ** 15, 2 ** 15, (6, kv, page, dim), dtype=np.int16) for _ in range(2))
+    kd.copy_(torch.from_numpy(k).view(torch.float16))
+    vd.copy_(torch.from_numpy(v).view(torch.float16))
+    table = np.array([[4, 0, 5]], np.int32)
+    cache = endor.KVCache(kd, vd, torch.from_numpy(table).cuda())
+    for tokens in (1, 8, 9):  # at the third page's end
+        new = torch.from_numpy(g.integers(-2 ** 15, 2 ** 15, (2, 1, tokens, kv, dim), dtype=np.int16)).view(torch.float16)
+        n, _ = endor.kv_append(cache, new[0].cuda(), new[1].cuda(), ints([length]))
+        assert n.tolist() == [length + tokens]
+        for pool, x in ((k, new[0]), (v, new[1])):
+            pool[5, 0, length - 256:length - 256 + tokens] = bits(x)[0, :, 0]
+        assert np.array_equal(bits(cache.k), k) and np.array_equal(bits(cache.v), v)
+    w = statistics(g, 1, kv, cache.capacity, "random")
+    pos = np.arange(cache.capacity, dtype=np.int32)[None, None].copy()
+    run_evict(np.array([380], np.int32), np.array([380], np.int32), w, pos, budget, 20, cache, k, v, table)
+
+
 def test_evict_bounds_and_missing_pages():
     lengths = np.array([-3, 100, 2 ** 31 - 1, 90], np.int32)
     cache, k, v, table, g = make(lengths, [16, 100, 112, 96], 2, 64, 16, seed=8, gaps=True)
