@@ -226,7 +226,8 @@ __device__ __forceinline__ void move_tokens(const Cache &C, const Move *moves, u
 // here.
 //
 // Bound by the passes one after the other, each of which the slowest wave ends, not by the 8 bytes a slot that it reads:
-// 16 x 8 rows of up to 16000 tokens 18 to 21 us, 13 x 16 of 6600 11.5, 8 x 72 of 3457 14.2 (3 TB/s by its bytes).
+// 16 x 8 rows of 16000 tokens 16.5 us, a third of it until the keys are there, a third the histograms, a third ranks and
+// lists; 13 x 16 of 6600 11.3, 8 x 72 of 3457 13.6.
 template <int kThreads, int kChunks, bool kMove>
 __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E) {
     constexpr uint32_t kWaves = kThreads / 64;
@@ -308,6 +309,25 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
     // What stays whatever it weighs; the least and the largest key of the others.
     // One is taken off or added so that neither what stays nor what is no token is the least or the largest.
     uint32_t staying = 0, low = 0xffffffffu, high = 0;
+    auto leave_ends = [&] {  // the wave's, for all
+#pragma unroll
+        for (int d = 32; d; d >>= 1) {
+            const uint32_t l = __shfl_xor(low, d), u = __shfl_xor(high, d);
+            low = l < low ? l : low;
+            high = u > high ? u : high;
+        }
+        if (lane == 0) {
+            S.low[wave] = low;
+            S.high[wave] = high;
+        }
+    };
+    auto take_ends = [&] {
+#pragma unroll
+        for (uint32_t v = 0; v < kWaves; ++v) {
+            low = S.low[v] < low ? S.low[v] : low;
+            high = S.high[v] > high ? S.high[v] : high;
+        }
+    };
     each([&](uint32_t, u32x4 key) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -316,43 +336,34 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
             high = key[e] + 1 > high ? key[e] + 1 : high;
         }
     });
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        const uint32_t l = __shfl_xor(low, d), u = __shfl_xor(high, d);
-        low = l < low ? l : low;
-        high = u > high ? u : high;
-    }
-    if (lane == 0) {
-        S.low[wave] = low;
-        S.high[wave] = high;
-    }
+    leave_ends();
     group_scan<kWaves>(staying, S, turn++, &total);  // its barrier is for both
     staying = total;
-#pragma unroll
-    for (uint32_t v = 0; v < kWaves; ++v) {
-        low = S.low[v] < low ? S.low[v] : low;
-        high = S.high[v] > high ? S.high[v] : high;
-    }
+    take_ends();
     ++low;
     --high;
     uint32_t least = kStay, ties = budget;  // keys above `least` stay, and the first `ties` of those equal to it
     // An eviction at every step has one token too many: the least key is known by now. 4 x 8 rows of 2049 tokens 5.8 us,
-    // 8.9 by the histograms; 32 x 8 of 4097 8.8 and 13.3.
+    // 7.9 by the histograms.
     const bool one_goes = staying < budget && length - budget == 1;
     if (one_goes) {
         least = low;  // and the last of its equals goes, once they are counted
     } else if (staying < budget) {
         uint32_t need = budget - staying;
         // more keys are left than are needed, so low <= high
-        const uint32_t range = high - low;
-        uint32_t shift = range >> kBinBits ? 32 - __clz(range) - kBinBits : 0;
-        uint32_t width = range + 1;  // keys in [low, low + width) are still in question: neither 0 nor what stays
         for (;;) {
+            const uint32_t range = high - low;  // keys in [low, high] are still in question: neither 0 nor what stays
+            const uint32_t shift = range >> kBinBits ? 32 - __clz(range) - kBinBits : 0;
+            uint32_t least_ones = 0;  // often many, weights of zero say, which would be added one after the other
             each([&](uint32_t, u32x4 key) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (key[e] - low < width) atomicAdd(&S.bins[(key[e] - low) >> shift], 1u);
+                for (int e = 0; e < 4; ++e) {
+                    least_ones += key[e] == low;
+                    if (key[e] - low - 1 < range) atomicAdd(&S.bins[(key[e] - low) >> shift], 1u);
+                }
             });
+            least_ones = wave_sum(least_ones);
+            if (lane == 0) atomicAdd(&S.bins[0], least_ones);
             __syncthreads();
             // from the top down
             const uint32_t top = kBins - 1 - kOwn * threadIdx.x;
@@ -383,8 +394,8 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
                 ties = shift == 0 ? need : 0xffffffffu;  // all of the bin stay: those from its lower end on
                 break;
             }
-            width = 1u << shift;
-            shift = shift > kBinBits ? shift - kBinBits : 0;
+            const uint32_t width = 1u << shift, from_low = low;
+            high = low + (width - 1);
             if (in_bin <= 64) {
                 each([&](uint32_t, u32x4 key) {
 #pragma unroll
@@ -409,6 +420,28 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
                 const uint32_t from = __builtin_ctzll(at);
                 least = __builtin_amdgcn_readlane(key, from);
                 ties = need - __builtin_amdgcn_readlane(over, from);
+                break;
+            }
+            // Many in one of so many bins are often one and the same key: the bin's own least and largest. A fifth of the
+            // weights zero and the last kept one among them: 6 rows of 23823 tokens 22.7 us, by the bins alone 32.1; 4 x 8
+            // of 2050 7.8 and 9.1; elsewhere it would cost 0.8.
+            if (in_bin < length / 16) continue;
+            low = 0xffffffffu;
+            high = 0;
+            each([&](uint32_t, u32x4 key) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool in = key[e] - from_low < width;
+                    low = in && key[e] < low ? key[e] : low;
+                    high = in && key[e] > high ? key[e] : high;
+                }
+            });
+            leave_ends();
+            __syncthreads();
+            take_ends();
+            if (low == high) {
+                least = low;
+                ties = need;
                 break;
             }
         }
@@ -532,10 +565,9 @@ __global__ __launch_bounds__(256) void endor_kv_shorten_kernel(EvictParams E) {
 // The chunks are the fewest that hold the tokens in registers. Small workgroups have fewer waves to
 // wait for at each barrier, and two of them share a compute unit better than two large ones do; large
 // ones hold more tokens and work longer rows off sooner where there is one for each unit at most.
-// Measured with 512 | 1024 threads: 1 x 8 rows of 1025 tokens 7.2 | 8.9 us, 4 x 8 of 2049 8.9 | 9.6,
-// 1 x 8 of 4000 10.0 | 10.7, 64 x 8 of 1025 9.7 | 17.6, 8 x 72 of 3457 14.2 | 24.2, 64 x 8 of 16000
-// 40.5 | 46.4; but 13 x 16 of 6600 12.7 | 11.5 and 32 x 8 of 4097 13.3 | 13.4. With 256 threads all
-// but the shortest rows take longer: 4 x 8 of 2049 10.8, 8 x 72 of 3457 16.8.
+// Measured with 512 | 1024 threads: 1 x 8 rows of 1026 tokens 6.5 | 8.0 us, 4 x 8 of 2050 7.9 | 8.3, 8 x 72 of 3457
+// 13.6 | 23.3, 64 x 8 of 8000 22.9 | 27.4, of 16000 39.1 | 45.0; but 13 x 16 of 6600 12.3 | 11.3 and 16 x 8 of 16000
+// 20.3 | 16.5. 256 threads take longer for all but the shortest rows.
 template <bool kMove>
 void launch_select(const EvictParams &E, hipStream_t s) {
     constexpr int kUnits = 256;
