@@ -166,6 +166,21 @@ def test_evict_long(length):
         run_evict(lengths, lengths.copy(), w, pos, length // 2, 100, cache, k, v, table)
 
 
+@pytest.mark.parametrize("length", [700, 2100, 5000, 9000, 40000])
+def test_evict_weights_close_together(length):
+    """Nearly all weights in one bin of the first pass, among them many equal ones, with far smaller and larger ones beside them."""
+    print("evict close", length, flush=True)
+    lengths = np.array([length, length], np.int32)
+    cache, k, v, table, g = make(lengths, lengths, 2, 8, 64, seed=length)
+    w = (1 + g.integers(0, 3000, (2, 2, cache.capacity)) * 2.0 ** -23).astype(np.float32)
+    w[:, :, ::7] = np.float32(1 + 1500 * 2.0 ** -23)
+    w[:, :, 3::101], w[:, :, 5::103], w[:, :, 9::211] = 0, 1e-30, 3e30
+    w[1, 1] = np.where(g.random(cache.capacity) < 0.8, 0, w[1, 1])
+    pos = np.broadcast_to(np.arange(cache.capacity, dtype=np.int32), w.shape).copy()
+    for budget in (length // 5, length // 2, length - length // 8, length - 2, length - 1):
+        run_evict(lengths, lengths.copy(), w, pos, budget, 10, cache, k, v, table)
+
+
 @pytest.mark.parametrize("batch,heads,length", [(3, 72, 5000), (4, 72, 5000), (4, 72, 9001), (9, 30, 16384), (9, 30, 16385), (300, 1, 513)])
 def test_evict_many_rows(batch, heads, length):
     """More rows than compute units, and fewer; with few moves and with many."""
