@@ -5,6 +5,7 @@
 
 #include "endor.h"
 #include "endor_device.h"
+#include "endor_evict_search.h"
 #include "endor_kv.h"
 
 namespace {
@@ -12,6 +13,12 @@ namespace {
 using endor_device::u32x4;
 using endor_device::wave_inclusive_scan;
 using endor_device::wave_sum;
+using endor_evict_search::Bin;
+using endor_evict_search::kBins;
+using endor_evict_search::kFew;
+using endor_evict_search::Last;
+using endor_evict_search::last_to_stay;
+using endor_evict_search::Range;
 using endor_kv::aligned;
 using endor_kv::Cache;
 using endor_kv::capacity_of;
@@ -149,8 +156,7 @@ __device__ __forceinline__ uint32_t key_of(float w, int32_t position, int64_t ne
     return bits >> 31 ? ~bits : bits | 0x80000000u;
 }
 
-constexpr int kMostWaves = 16;                       // of a workgroup that selects
-constexpr int kBinBits = 11, kBins = 1 << kBinBits;  // of a pass over the keys
+constexpr int kMostWaves = 16;  // of a workgroup that selects
 
 // Where a token's keys and values are and go: element offsets from the pools' beginnings; -1 where a page is not there.
 struct Move {
@@ -170,9 +176,17 @@ struct SelectShared {
     uint32_t part[2][kMostWaves];
     uint32_t low[kMostWaves], high[kMostWaves];
     uint32_t found[3];  // the bin that the last kept key is in, the keys above it, the keys in it
-    uint32_t left, last[64], over[64], same[64];  // the keys in question, when a wave can hold them; the keys above each and its equals
+    uint32_t left, last[kFew], over[kFew], same[kFew];  // the keys in question, when a wave can hold them; the keys above each and its equals
     int32_t holes[kFewMoves], movers[kFewMoves];
     Move moves[kFewMoves];
+};
+
+// The passes of the search for the last key that stays.
+template <class Count, class Rank, class Ends>
+struct Passes {
+    Count count;
+    Rank rank;
+    Ends ends;
 };
 
 // Exclusive prefix over the workgroup, and the total. `turn` changes from one call to the next, so that one barrier
@@ -276,7 +290,7 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
     };
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) S.bins[threadIdx.x + i * kThreads] = 0;
-    if (threadIdx.x < 64) S.over[threadIdx.x] = S.same[threadIdx.x] = 0;
+    if (threadIdx.x < kFew) S.over[threadIdx.x] = S.same[threadIdx.x] = 0;
     if (threadIdx.x == 0) S.left = 0;
     u32x4 held[kChunks ? kChunks : 1];
     if constexpr (kChunks > 0)
@@ -349,17 +363,14 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
     if (one_goes) {
         least = low;  // and the last of its equals goes, once they are counted
     } else if (staying < budget) {
-        uint32_t need = budget - staying;
-        // more keys are left than are needed, so low <= high
-        for (;;) {
-            const uint32_t range = high - low;  // keys in [low, high] are still in question: neither 0 nor what stays
-            const uint32_t shift = range >> kBinBits ? 32 - __clz(range) - kBinBits : 0;
+        auto count = [&](const Range &r, uint32_t bits) {
+            const uint32_t range = r.high - r.low;
             uint32_t least_ones = 0;  // often many, weights of zero say, which would be added one after the other
             each([&](uint32_t, u32x4 key) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    least_ones += key[e] == low;
-                    if (key[e] - low - 1 < range) atomicAdd(&S.bins[(key[e] - low) >> shift], 1u);
+                    least_ones += key[e] == r.low;
+                    if (key[e] - r.low - 1 < range) atomicAdd(&S.bins[r.bin_of(key[e], bits)], 1u);
                 }
             });
             least_ones = wave_sum(least_ones);
@@ -375,10 +386,10 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
                 sum += own[i];
             }
             uint32_t above = group_scan<kWaves>(sum, S, turn++, &total);
-            if (above < need && above + sum >= need)
+            if (above < r.need && above + sum >= r.need)
 #pragma unroll
                 for (int i = 0; i < kOwn; ++i) {
-                    if (above < need && above + own[i] >= need) {
+                    if (above < r.need && above + own[i] >= r.need) {
                         S.found[0] = top - i;
                         S.found[1] = above;
                         S.found[2] = own[i];
@@ -386,52 +397,39 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
                     above += own[i];
                 }
             __syncthreads();
-            const uint32_t in_bin = S.found[2];
-            low += S.found[0] << shift;
-            need -= S.found[1];
-            if (shift == 0 || need == in_bin) {
-                least = low;
-                ties = shift == 0 ? need : 0xffffffffu;  // all of the bin stay: those from its lower end on
-                break;
-            }
-            const uint32_t width = 1u << shift, from_low = low;
-            high = low + (width - 1);
-            if (in_bin <= 64) {
-                each([&](uint32_t, u32x4 key) {
+            return Bin{S.found[0], S.found[1], S.found[2]};
+        };
+        auto rank = [&](const Range &r, uint32_t in_bin) {
+            each([&](uint32_t, u32x4 key) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (key[e] - low < width) S.last[atomicAdd(&S.left, 1u)] = key[e];
-                });
-                __syncthreads();
-                const uint32_t key = lane < in_bin ? S.last[lane] : 0;
-                uint32_t over = 0, same = 0;
-                for (uint32_t i = wave; i < in_bin; i += kWaves) {
-                    const uint32_t other = S.last[i];
-                    over += other > key;
-                    same += other == key;
-                }
-                atomicAdd(&S.over[lane], over);
-                atomicAdd(&S.same[lane], same);
-                __syncthreads();
-                over = S.over[lane];
-                same = S.same[lane];
-                // the lanes that hold the last key to stay; all waves find the same
-                const uint64_t at = __ballot(lane < in_bin && over < need && over + same >= need);
-                const uint32_t from = __builtin_ctzll(at);
-                least = __builtin_amdgcn_readlane(key, from);
-                ties = need - __builtin_amdgcn_readlane(over, from);
-                break;
+                for (int e = 0; e < 4; ++e)
+                    if (r.holds(key[e])) S.last[atomicAdd(&S.left, 1u)] = key[e];
+            });
+            __syncthreads();
+            const uint32_t key = lane < in_bin ? S.last[lane] : 0;
+            uint32_t over = 0, same = 0;
+            for (uint32_t i = wave; i < in_bin; i += kWaves) {
+                const uint32_t other = S.last[i];
+                over += other > key;
+                same += other == key;
             }
-            // Many in one of so many bins are often one and the same key: the bin's own least and largest. A fifth of the
-            // weights zero and the last kept one among them: 6 rows of 23823 tokens 22.7 us, by the bins alone 32.1; 4 x 8
-            // of 2050 7.8 and 9.1; elsewhere it would cost 0.8.
-            if (in_bin < length / 16) continue;
+            atomicAdd(&S.over[lane], over);
+            atomicAdd(&S.same[lane], same);
+            __syncthreads();
+            over = S.over[lane];
+            same = S.same[lane];
+            // the lanes that hold the last key to stay; all waves find the same
+            const uint64_t at = __ballot(lane < in_bin && over < r.need && over + same >= r.need);
+            const uint32_t from = __builtin_ctzll(at);
+            return Last{uint32_t(__builtin_amdgcn_readlane(key, from)), r.need - __builtin_amdgcn_readlane(over, from)};
+        };
+        auto ends = [&](Range *r) {
             low = 0xffffffffu;
             high = 0;
             each([&](uint32_t, u32x4 key) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const bool in = key[e] - from_low < width;
+                    const bool in = r->holds(key[e]);
                     low = in && key[e] < low ? key[e] : low;
                     high = in && key[e] > high ? key[e] : high;
                 }
@@ -439,12 +437,15 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
             leave_ends();
             __syncthreads();
             take_ends();
-            if (low == high) {
-                least = low;
-                ties = need;
-                break;
-            }
-        }
+            r->low = low;
+            r->high = high;
+        };
+        // More keys are left than are needed, so low <= high. A bin's own ends cost a pass: a fifth of the weights zero and
+        // the last kept one among them, 6 rows of 23823 tokens 22.7 us, by the bins alone 32.1; 4 x 8 of 2050 7.8 and 9.1;
+        // where bins hold less it would cost 0.8.
+        const Last last = last_to_stay(Range{low, high, budget - staying}, length / 16, Passes<decltype(count), decltype(rank), decltype(ends)>{count, rank, ends});
+        least = last.key;
+        ties = last.ties;
     }
 
     // Which stay: above, or equal and among the first. Of the waves before this one: equal keys, then slots that come
