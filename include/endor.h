@@ -488,7 +488,7 @@ typedef struct endor_kv_cache {
  *                     (the cache's type, element-aligned; strides in elements)
  *   d_counts          [batch] or NULL: every sequence brings `tokens`
  *   d_lengths, d_seen [batch]: slots in use, and tokens seen so far (more than lengths after eviction)
- *   d_lengths_out, d_seen_out   [batch]: both advanced by the tokens stored; may be the arrays above
+ *   d_lengths_out, d_seen_out   [batch]: both advanced by the tokens stored; may be the arrays above, which may be one
  *   d_weights, d_positions      [batch][kv_heads][capacity] or NULL: the new slots' weight is set to 0,
  *                     their position to seen[b] + t
  * Tokens past the capacity are not stored.  Pages that a sequence appends to must be its own.

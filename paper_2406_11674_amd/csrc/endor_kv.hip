@@ -127,9 +127,10 @@ __global__ __launch_bounds__(256) void endor_kv_append_many_kernel(AppendParams 
 __global__ __launch_bounds__(256) void endor_kv_advance_kernel(AppendParams A) {
     const int32_t b = blockIdx.x * 256 + threadIdx.x;
     if (b >= A.C.batch) return;
-    const uint32_t length = clamp_length(A.lengths[b], A.capacity), stored = stored_of(A, b, length);
+    // both before either is stored: all four may be one array
+    const uint32_t length = clamp_length(A.lengths[b], A.capacity), seen = A.seen[b], stored = stored_of(A, b, length);
     A.lengths_out[b] = length + stored;
-    A.seen_out[b] = A.seen[b] + stored;
+    A.seen_out[b] = seen + stored;
 }
 
 // ---------------------------------------------------------------- evict
