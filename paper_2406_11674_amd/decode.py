@@ -98,7 +98,8 @@ class KVCache:
             raise ValueError("k and v must be alike, [pages, kv_heads, page_size, head_dim], on the table's device")
         if pages.dtype != torch.int32 or pages.dim() != 2 or (pages.shape[1] > 1 and pages.stride(1) != 1):
             raise ValueError("pages must be an int32 tensor [batch, max_pages] with contiguous rows")
-        if any(n > 1 and a != b for n, a, b in zip(k.shape, k.stride(), v.stride())) or (k.shape[3] > 1 and k.stride(3) != 1):
+        empty = k.numel() == 0
+        if not empty and (any(n > 1 and a != b for n, a, b in zip(k.shape, k.stride(), v.stride())) or (k.shape[3] > 1 and k.stride(3) != 1)):
             raise ValueError("k and v must have the same strides, the last one 1")
         if not k.is_cuda:
             raise ValueError("the cache lies in GPU memory")
@@ -108,8 +109,8 @@ class KVCache:
         self.capacity = self.max_pages * self.page_size
         c = self._c = _Cache()
         c.d_k, c.d_v, c.d_pages = _dptr(k), _dptr(v), _dptr(pages)
-        # the stride over a dimension of one element is never used, whatever torch says it is
-        c.page_stride, c.head_stride, c.slot_stride = (int(k.stride(i)) if k.shape[i] > 1 else -(-self.head_dim // 8) * 8 for i in range(3))
+        # the stride over a dimension of one element is never used, whatever torch says it is, and an empty pool's are not either
+        c.page_stride, c.head_stride, c.slot_stride = (int(k.stride(i)) if k.shape[i] > 1 and not empty else -(-self.head_dim // 8) * 8 for i in range(3))
         c.num_pages, c.pages_stride = self.num_pages, int(pages.stride(0)) if self.batch > 1 else self.max_pages
         c.batch, c.kv_heads, c.head_dim, c.page_size, c.max_pages = self.batch, self.kv_heads, self.head_dim, self.page_size, self.max_pages
         c.dtype = _dtype_code(k.dtype)
