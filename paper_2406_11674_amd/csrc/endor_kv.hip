@@ -212,7 +212,7 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t x, SelectShared &S, uint
 __device__ __forceinline__ void move_tokens(const Cache &C, const Move *moves, uint32_t count, uint32_t threads) {
     const uint32_t half = C.dim / 8, per = 2 * half, lines = threads / per, line = threadIdx.x / per, part = threadIdx.x % per;
     uint16_t *pool = (part < half ? C.k : C.v) + 8 * (part < half ? part : part - half);
-    if (line >= lines) return;
+    if (line >= lines || C.num_pages == 0) return;  // a pool without pages may be no memory at all
     for (uint32_t i0 = line; i0 < count; i0 += 4 * lines) {
         u32x4 held[4];
         int64_t to[4];
@@ -221,7 +221,7 @@ __device__ __forceinline__ void move_tokens(const Cache &C, const Move *moves, u
             const uint32_t i = i0 + k * lines;
             const Move m = moves[i < count ? i : i0];
             to[k] = i < count ? m.to : -1;
-            held[k] = *reinterpret_cast<const u32x4 *>(pool + (m.from < 0 ? 0 : m.from));  // the pool has a first page: something is to be moved
+            held[k] = *reinterpret_cast<const u32x4 *>(pool + (m.from < 0 ? 0 : m.from));  // the first page is there
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k)
