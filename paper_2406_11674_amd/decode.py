@@ -22,13 +22,16 @@ class _Cache(ctypes.Structure):
 
 _lib_declared = None
 _torch_module = None
+_current_gpu = None
 
 
 def _torch():
-    global _torch_module
+    global _torch_module, _current_gpu
     if _torch_module is None:
         import torch
         _torch_module = torch
+        # not part of torch's interface: 0.1 us for 0.24
+        _current_gpu = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     return _torch_module
 
 
@@ -64,6 +67,14 @@ def _stream(stream, device):
         return _torch_module._C._cuda_getCurrentRawStream(device)  # not part of torch's interface: 0.2 us for 2.9
     except AttributeError:
         return int(_torch().cuda.current_stream(device).cuda_stream)
+
+
+def _on(device, entry):
+    """The library's entry point, called with that GPU as the current one."""
+    def there(*args):
+        with _torch().cuda.device(device):
+            return entry(*args)
+    return there
 
 
 # The checks of a call are on the way of every token, and a tensor's attributes take 50 ns each: they are asked for
@@ -178,10 +189,12 @@ def kv_append(cache, k, v, lengths, seen=None, counts=None, weights=None, positi
         cache._per_slot(torch.float32, weights)
     if positions is not None:
         cache._per_slot(torch.int32, positions)
-    status = _lib().endor_kv_append(cache._at, k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], tokens, None if counts is None else counts.data_ptr(),
-                                    lengths.data_ptr(), seen.data_ptr(), new_lengths.data_ptr(), new_seen.data_ptr(),
-                                    None if weights is None else weights.data_ptr(), None if positions is None else positions.data_ptr(),
-                                    _stream(stream, device))
+    entry = _lib().endor_kv_append
+    if _current_gpu() != device:
+        entry = _on(device, entry)
+    status = entry(cache._at, k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], tokens, None if counts is None else counts.data_ptr(),
+                   lengths.data_ptr(), seen.data_ptr(), new_lengths.data_ptr(), new_seen.data_ptr(),
+                   None if weights is None else weights.data_ptr(), None if positions is None else positions.data_ptr(), _stream(stream, device))
     if status:
         _check(status, "endor_kv_append")
     return new_lengths, new_seen
@@ -227,10 +240,13 @@ def attn_decode(cache, q, lengths, max_len=None, mask=None, scale=None, weights=
     if lse.dtype is not torch.float32 or lse.numel() != batch * q_heads or lse.get_device() != device or not lse.is_contiguous():
         _bad("lse must be a contiguous float32 tensor [batch, q_heads]")
     scratch_at, room = cache._take(scratch)
-    status = _lib().endor_attn_decode(cache._at, q_heads, q.data_ptr(), st[0], st[1], lengths.data_ptr(), max_len, mask_at, mask_stride,
-                                      cache.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr(),
-                                      None if weights is None else weights.data_ptr(), None if new_weights is None else new_weights.data_ptr(),
-                                      scratch_at, room, _stream(stream, device))
+    entry = _lib().endor_attn_decode
+    if _current_gpu() != device:
+        entry = _on(device, entry)
+    status = entry(cache._at, q_heads, q.data_ptr(), st[0], st[1], lengths.data_ptr(), max_len, mask_at, mask_stride,
+                   cache.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr(),
+                   None if weights is None else weights.data_ptr(), None if new_weights is None else new_weights.data_ptr(),
+                   scratch_at, room, _stream(stream, device))
     if status:
         _check(status, "endor_attn_decode")
     return out, lse
@@ -253,9 +269,13 @@ def kv_evict(cache, lengths, seen, weights, positions, budget, recent, max_len=N
     cache._per_slot(torch.float32, weights, new_weights)
     cache._per_slot(torch.int32, positions, new_positions)
     scratch_at, room = cache._take(scratch)
-    status = _lib().endor_kv_evict(cache._at, budget, recent, max_len, lengths.data_ptr(), seen.data_ptr(), weights.data_ptr(), positions.data_ptr(),
-                                   new_lengths.data_ptr(), new_weights.data_ptr(), new_positions.data_ptr(), scratch_at, room,
-                                   _stream(stream, cache.device_index))
+    device = cache.device_index
+    entry = _lib().endor_kv_evict
+    if _current_gpu() != device:
+        entry = _on(device, entry)
+    status = entry(cache._at, budget, recent, max_len, lengths.data_ptr(), seen.data_ptr(), weights.data_ptr(),
+                   positions.data_ptr(), new_lengths.data_ptr(), new_weights.data_ptr(), new_positions.data_ptr(),
+                   scratch_at, room, _stream(stream, device))
     if status:
         _check(status, "endor_kv_evict")
     return new_lengths, new_weights, new_positions
@@ -302,7 +322,11 @@ def q4_pack(codes, scales, zeros, cols, group, stream=None):
     L = _lib()
     with _of(stream):
         packed = torch.empty(L.endor_q4_bytes(rows, cols, group, int(zeros is not None)), dtype=torch.uint8, device=codes.device)
-    _check(L.endor_q4_pack(rows, cols, group, _dptr(codes), _dptr(scales), _dptr(zeros), _dptr(packed), packed.numel(), _stream(stream, codes.get_device())),
+    device = codes.get_device()
+    entry = L.endor_q4_pack
+    if _current_gpu() != device:
+        entry = _on(device, entry)
+    _check(entry(rows, cols, group, _dptr(codes), _dptr(scales), _dptr(zeros), _dptr(packed), packed.numel(), _stream(stream, device)),
            "endor_q4_pack")
     return Q4Matrix(rows, cols, group, zeros is not None, packed)
 
@@ -321,7 +345,11 @@ def q4_quantize(dense, group=128, zeros=False, stream=None):
         codes = torch.empty((rows, (cols + 1) // 2), dtype=torch.uint8, device=dense.device)
         scales = torch.empty((rows, _q4_groups(cols, group)), dtype=torch.float16, device=dense.device)
         points = torch.empty(scales.shape, dtype=torch.uint8, device=dense.device) if zeros else None
-    _check(_lib().endor_q4_quantize(rows, cols, group, _dptr(dense), _dptr(codes), _dptr(scales), _dptr(points), _stream(stream, dense.get_device())),
+    device = dense.get_device()
+    entry = _lib().endor_q4_quantize
+    if _current_gpu() != device:
+        entry = _on(device, entry)
+    _check(entry(rows, cols, group, _dptr(dense), _dptr(codes), _dptr(scales), _dptr(points), _stream(stream, device)),
            "endor_q4_quantize")
     return codes, scales, points
 
@@ -356,8 +384,11 @@ def q4_gemm(m, X, Y=None, scratch=None, stream=None):
         _bad("scratch must be contiguous, on the weight's GPU")
     if scratch is not None:
         scratch_at, space = scratch.data_ptr(), scratch.numel() * scratch.element_size()
-    status = _lib().endor_q4_gemm(rows, cols, m.group, m.zeros, at, room, 0 if dtype is torch.float16 else _dtype_code(dtype), X.data_ptr(),
-                                  ldx if nb > 1 else cols, nb, Y.data_ptr(), scratch_at, space, _stream(stream, device))
+    entry = _lib().endor_q4_gemm
+    if _current_gpu() != device:
+        entry = _on(device, entry)
+    status = entry(rows, cols, m.group, m.zeros, at, room, 0 if dtype is torch.float16 else _dtype_code(dtype), X.data_ptr(),
+                   ldx if nb > 1 else cols, nb, Y.data_ptr(), scratch_at, space, _stream(stream, device))
     if status:
         _check(status, "endor_q4_gemm")
     return Y
