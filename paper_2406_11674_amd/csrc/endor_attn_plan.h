@@ -32,6 +32,7 @@ inline Plan make_plan(int batch, int kv_heads, int q_heads, int dim, int32_t max
     p.units = static_cast<uint32_t>(kv_heads) * p.qtiles;
     p.row = static_cast<int32_t>((int64_t(max_len) + 63) / 64 * 64);
     const int64_t units = int64_t(batch) * p.units;
+    if (units == 0) return p;  // no sequences
     // One launch where a compute unit reads its share in about the time of the second one (1024 slots of one head of
     // 64, or 512 of 128: 8.6 us in one launch, 8.8 in two; 1024 of 128 17.8 and 10.8), or where the units fill half of
     // the chip by themselves (256 of 1000 slots: 24.7 and 29.5).
