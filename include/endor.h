@@ -515,7 +515,9 @@ endor_status endor_kv_append(const endor_kv_cache *cache, const void *d_k_new, c
  *                over the query heads that share the kv head, for all t < min(lengths[b], max_len); slots past that
  *                are left alone.  d_weights may be d_weights_out, or NULL (then taken as 0).
  *   d_scratch    endor_attn_scratch_bytes() bytes, 256-byte aligned (NULL when that is 0)
- * q_heads is a multiple of kv_heads.  A visible slot whose key or value is not finite makes outputs that are not finite.
+ * q_heads is a multiple of kv_heads.  A slot whose logit is -infinity weighs nothing, as one that is not visible.  A logit
+ * of +infinity or NaN makes the outputs of its query head and the weights_out of its kv head NaN; a visible slot's value
+ * that is not finite makes its element of the outputs not finite, whatever the slot weighs.
  */
 size_t endor_attn_scratch_bytes(const endor_kv_cache *cache, int q_heads, int32_t max_len, int with_weights);
 endor_status endor_attn_decode(const endor_kv_cache *cache, int q_heads,
