@@ -556,7 +556,8 @@ endor_status endor_kv_evict(const endor_kv_cache *cache, int32_t budget, int32_t
  * endor_q4_pack into endor_q4_bytes() bytes (256-byte aligned; 0 on bad arguments).  rows*cols < 2^34, rows and cols < 2^26.
  *
  * endor_q4_quantize makes a checkpoint's form of a dense fp16 matrix (rows*cols elements, contiguous) by rounding to
- * nearest: with d_zeros from the smallest and largest value of a group (0 among them), without symmetrically.
+ * nearest: with d_zeros from the smallest and largest value of a group (0 among them), without symmetrically.  The values
+ * are finite: 4 bits have no code for others (a NaN gets the lowest one, an infinity makes its group's scale infinite).
  */
 size_t endor_q4_bytes(int64_t rows, int64_t cols, int group, int with_zeros);
 endor_status endor_q4_pack(int64_t rows, int64_t cols, int group, const uint8_t *d_codes, const uint16_t *d_scales,
@@ -570,7 +571,7 @@ endor_status endor_q4_quantize(int64_t rows, int64_t cols, int group, const uint
  *   d_y      out, nb x rows fp32: the sums of (code - zero)*x over a group are exact products summed in fp32, then
  *            multiplied by the group's scale and summed in fp32, in a fixed order: results are the same from run to run
  *   d_scratch  endor_q4_scratch_bytes() bytes, 256-byte aligned (NULL when that is 0): sums of parts of the columns
- * 16-byte aligned d_x with ldx a multiple of 8 selects the fast load path.
+ * d_x need only be aligned to its elements, and any ldx will do: all take the same path.
  */
 size_t endor_q4_scratch_bytes(int64_t rows, int64_t cols, int group, int nb);
 endor_status endor_q4_gemm(int64_t rows, int64_t cols, int group, int with_zeros, const void *d_packed, size_t packed_bytes,
