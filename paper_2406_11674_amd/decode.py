@@ -305,8 +305,8 @@ def q4_pack(codes, scales, zeros, cols, group, stream=None):
     """endor_q4_pack.  codes: uint8 [rows, (cols + 1) // 2], the even column in the low half; scales: float16 [rows, ceil(cols / group)];
     zeros: uint8 of that shape, or None for 8 everywhere.  Returns a Q4Matrix."""
     torch = _torch()
-    if group < 1:
-        raise ValueError("group must be a power of two from 32 on")
+    if not 1 <= group <= 0x7fffffff:  # the library gets its low 32 bits, by which it counts the groups of a row
+        raise ValueError("group must be a power of two from 32 to 32768")
     rows = int(codes.shape[0])
     if codes.dtype != torch.uint8 or tuple(codes.shape) != (rows, (cols + 1) // 2) or not codes.is_contiguous():
         raise ValueError("codes must be a contiguous uint8 tensor [rows, (cols + 1) // 2]")
@@ -339,8 +339,8 @@ def q4_quantize(dense, group=128, zeros=False, stream=None):
     rows, cols = (int(n) for n in dense.shape)
     if not dense.is_cuda:
         raise ValueError("dense must lie in GPU memory")
-    if group < 1:
-        raise ValueError("group must be a power of two from 32 on")
+    if not 1 <= group <= 0x7fffffff:  # the library gets its low 32 bits, by which it counts the groups of a row
+        raise ValueError("group must be a power of two from 32 to 32768")
     with _of(stream):
         codes = torch.empty((rows, (cols + 1) // 2), dtype=torch.uint8, device=dense.device)
         scales = torch.empty((rows, _q4_groups(cols, group)), dtype=torch.float16, device=dense.device)
