@@ -89,6 +89,11 @@ def _bad(what):
     raise ValueError(what)
 
 
+def _saturated(n):
+    """A bound as the library gets it: 32 bits, and still above or below all that it is compared with."""
+    return max(-1, min(n, 0x7fffffff))
+
+
 def _dtype_code(dtype):
     torch = _torch()
     if dtype is torch.float16:
@@ -133,11 +138,11 @@ class KVCache:
 
     def attn_scratch(self, q_heads, max_len=None, weights=False):
         """Scratch of attn_decode for calls with these bounds; None if it takes none.  Calls that overlap in time need distinct ones."""
-        return self._scratch(_lib().endor_attn_scratch_bytes(self._at, q_heads, self.capacity if max_len is None else max_len, int(weights)))
+        return self._scratch(_lib().endor_attn_scratch_bytes(self._at, q_heads, self.capacity if max_len is None else _saturated(max_len), int(weights)))
 
     def evict_scratch(self, budget, max_len=None):
         """Scratch of kv_evict, likewise."""
-        return self._scratch(_lib().endor_kv_evict_scratch_bytes(self._at, budget, self.capacity if max_len is None else max_len))
+        return self._scratch(_lib().endor_kv_evict_scratch_bytes(self._at, _saturated(budget), self.capacity if max_len is None else _saturated(max_len)))
 
     def _per_sequence(self, *tensors):
         i32, batch, device = _torch_module.int32, self.batch, self.device_index
@@ -208,7 +213,7 @@ def attn_decode(cache, q, lengths, max_len=None, mask=None, scale=None, weights=
     Returns (out, lse)."""
     torch = _torch()
     batch, device = cache.batch, cache.device_index
-    max_len = cache.capacity if max_len is None else max_len
+    max_len = cache.capacity if max_len is None else max_len if -1 <= max_len <= 0x7fffffff else _saturated(max_len)
     shape = q.shape
     if len(shape) != 3 or q.dtype is not cache.dtype or q.get_device() != device or shape[0] != batch or shape[2] != cache.head_dim:
         _bad("q must be [batch, q_heads, head_dim] of the cache's type, on its GPU")
@@ -258,6 +263,8 @@ def kv_evict(cache, lengths, seen, weights, positions, budget, recent, max_len=N
     Returns (new_lengths, new_weights, new_positions); pass the inputs for them to change in place."""
     torch = _torch()
     max_len = cache.capacity if max_len is None else max_len
+    if not -1 <= max_len <= 0x7fffffff >= budget >= recent >= -1:
+        budget, recent, max_len = _saturated(budget), _saturated(recent), _saturated(max_len)
     if new_lengths is None or new_weights is None or new_positions is None or scratch is None:
         with _of(stream):
             new_lengths = torch.empty_like(lengths) if new_lengths is None else new_lengths
