@@ -79,7 +79,8 @@ class DecodeLayer:
         self.evict_scratch = self.cache.evict_scratch(budget, self.cache.capacity) if budget is not None else None
 
     def prompt(self, x, counts=None):
-        """Keys and values of prompts [batch, tokens, hidden]; sequence b brings counts[b] of the tokens."""
+        """Keys and values of prompts [batch, tokens, hidden]; sequence b brings counts[b] of the tokens.  No token attends to them yet, so their
+        weights are all zero: of a prompt longer than the budget the newest tokens stay, and beside them the first."""
         tokens = x.shape[1]
         k, v = (torch.stack([w(x[:, t].contiguous()) for t in range(tokens)], dim=1).view(self.batch, tokens, self.kv_heads, self.dim)
                 for w in (self.wk, self.wv))

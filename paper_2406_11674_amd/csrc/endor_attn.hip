@@ -445,8 +445,8 @@ __global__ __launch_bounds__(64 * kWaves) void endor_attn_kernel(AttnParams A, u
 // many let the short ones fill in behind the long (32 sequences of up to 4096: 54 us, 72 uncut). (Workgroups or waves
 // that stay and share out all tiles evenly were slower: on pages of their own, or by what finding their places costs.)
 //
-// Bound by memory where sequences are alike: 131072 slots of 8 heads of 128 take 82 us, 6.5 TB/s of the 6.6 that streamed
-// reads reach. Where they are not, by the compute units that have more than the mean at the end, and some 9 us in which
+// Bound by memory where sequences are alike: 131072 slots of 8 heads of 128 take 86 us in a trace, 6.2 TB/s of the 6.6
+// that streamed reads reach. Where they are not, by the compute units that have more than the mean at the end, and some 9 us in which
 // the first tiles are waited for and the waves joined: 48 sequences of 0 to 4001 slots, 8 heads of 64, 42 us for 158 MB.
 struct Part {
     uint32_t count, first, past;  // parts of the sequence; tiles of this one
@@ -501,6 +501,8 @@ __device__ __forceinline__ Part part_of(uint32_t length, uint32_t chunk, uint32_
     return {count, first, first + each + (s < more ? 1 : 0)};
 }
 
+// (Three waves to a SIMD leave heads of 65 to 128 three registers too few: two of them are read back in the loop, where
+// logits are stored.)
 template <int kDim, int kSub, int kWaves, bool kBf16>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kDim == 256 ? 1 : 3))) void endor_attn_part_kernel(AttnParams A) {
     typedef Tiles<kDim, kSub, kBf16> T;

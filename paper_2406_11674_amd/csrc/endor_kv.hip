@@ -110,8 +110,9 @@ __global__ __launch_bounds__(1024) void endor_kv_append_kernel(AppendParams A) {
 constexpr uint32_t kTokensEach = 8;
 
 // Prompts: kTokensEach tokens of a few heads a workgroup, so that a thread has four units of a head's. A second launch
-// advances the lengths where they may be read and written in one place. Bound by memory: 1777 tokens at most for each of
-// 4 sequences, 72 heads of 128, 299 MB read and written in 66 us, 4.5 TB/s (a large copy here: 4.8).
+// advances the lengths where they may be read and written in one place. 1777 tokens at most for each of 4
+// sequences, 72 heads of 128: 299 MB read and written in 66 us, 4.5 TB/s. A large copy by streamed loads and stores
+// reaches 6.6; the stores here are plain.
 __global__ __launch_bounds__(256) void endor_kv_append_many_kernel(AppendParams A, uint32_t heads_each) {
     const uint32_t b = blockIdx.z, first = blockIdx.x * kTokensEach, head0 = blockIdx.y * heads_each;
     const uint32_t length = clamp_length(A.lengths[b], A.capacity), stored = stored_of(A, b, length), heads = A.C.kv_heads;
@@ -241,7 +242,7 @@ __device__ __forceinline__ void move_tokens(const Cache &C, const Move *moves, u
 // here.
 //
 // Bound by the passes one after the other, each of which the slowest wave ends, not by the 8 bytes a slot that it reads:
-// 16 x 8 rows of 16000 tokens 16.5 us, a third of it until the keys are there, a third the histograms, a third ranks and
+// 16 x 8 rows of 16000 tokens 17 us, a third of it until the keys are there, a third the histograms, a third ranks and
 // lists; 13 x 16 of 6600 11.3, 8 x 72 of 3457 13.6.
 template <int kThreads, int kChunks, bool kMove>
 __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E) {
@@ -540,8 +541,9 @@ __global__ __launch_bounds__(kThreads) void endor_kv_select_kernel(EvictParams E
 
 constexpr int kMovesEach = 64;  // of a workgroup of the move kernel
 
-// Keys and values of the kept tokens past the budget. Bound by memory, as a copy of rows of 128 to 512 bytes in no order:
-// 8 x 72 rows that move 860 tokens of 64 dims each, 255 MB read and written in 59 us, 4.3 TB/s.
+// Keys and values of the kept tokens past the budget. 8 x 72 rows that move 860 tokens of 64 dims each: 255 MB read and
+// written in 59 us, 4.3 TB/s, where a large copy by streamed loads and stores reaches 6.6. Rows are of 128 to 512 bytes in
+// no order, and loads and stores are plain; how much either costs was not measured.
 __global__ __launch_bounds__(256) void endor_kv_move_kernel(EvictParams E) {
     __shared__ Move s_moves[kMovesEach];
     const uint32_t b = blockIdx.z, h = blockIdx.y, first = blockIdx.x * kMovesEach;
@@ -568,8 +570,8 @@ __global__ __launch_bounds__(256) void endor_kv_shorten_kernel(EvictParams E) {
 // wait for at each barrier, and two of them share a compute unit better than two large ones do; large
 // ones hold more tokens and work longer rows off sooner where there is one for each unit at most.
 // Measured with 512 | 1024 threads: 1 x 8 rows of 1026 tokens 6.5 | 8.0 us, 4 x 8 of 2050 7.9 | 8.3, 8 x 72 of 3457
-// 13.6 | 23.3, 64 x 8 of 8000 22.9 | 27.4, of 16000 39.1 | 45.0; but 13 x 16 of 6600 12.3 | 11.3 and 16 x 8 of 16000
-// 20.3 | 16.5. 256 threads take longer for all but the shortest rows.
+// 13.6 | 23.3, 64 x 8 of 8000 22.9 | 27.4, of 16000 39.1 | 45.0; but 13 x 16 of 6600 12.3 | 11.2 and 16 x 8 of 16000
+// 22 | 17. 256 threads take longer for all but the shortest rows.
 template <bool kMove>
 void launch_select(const EvictParams &E, hipStream_t s) {
     constexpr int kUnits = 256;

@@ -73,8 +73,9 @@ __device__ __forceinline__ uint32_t even_below_odd(uint32_t x) {
     return squeeze(x) | squeeze(x >> 4) << 16;
 }
 
-// A thread makes a lane's 16 bytes of a block; the first ones of a workgroup the scales and zeros. Bound by memory: 28672 x
-// 8192, 242 MB read and written in 67 us.
+// A thread makes a lane's 16 bytes of a block; the first ones of a workgroup the scales and zeros. 28672 x 8192 in groups
+// of 64: 242 MB read and written in 67 to 74 us, 3.3 to 3.6 TB/s, half of what a copy reaches: a load takes 16 bytes each of
+// 16 rows. Done once for a weight.
 __global__ __launch_bounds__(256) void endor_q4_pack_kernel(PackParams P) {
     const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, units = P.tiles * P.blocks * 64;
     if (i < units) {
@@ -113,8 +114,9 @@ __global__ __launch_bounds__(256) void endor_q4_pack_kernel(PackParams P) {
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
 // kLanes lanes for a row's group, eight columns to a lane at a time: a group of up to 512 in one go. The scale is rounded
-// to fp16 before the codes are taken, so that they are the nearest to what they stand for. Bound by memory: 8192 x 8192 in groups of
-// 128 52 us, 28672 x 8192 of 64 with zeros 199, 595 MB read and written.
+// to fp16 before the codes are taken, so that they are the nearest to what they stand for. 8192 x 8192 in groups of 128 52 to 56 us,
+// 28672 x 8192 of 64 with zeros 199: 595 MB read and written at 3.0 TB/s, less than half of what a copy reaches. Done once for a
+// weight.
 template <uint32_t kLanes>
 __global__ __launch_bounds__(256) void endor_q4_quantize_kernel(const _Float16 *dense, uint32_t first, uint32_t count, int64_t cols, int64_t group,
                                                                 uint32_t groups, uint8_t *codes, _Float16 *scales, uint8_t *zeros) {
@@ -331,7 +333,7 @@ __device__ __forceinline__ u32x4 columns_of(const uint16_t *x, int64_t c, int64_
 
 // Few right-hand sides: all of x lies in LDS, in the order of the operands, [block][32 columns][quarter][right-hand
 // side][8 columns]. A workgroup has one row tile, its waves take the blocks in turn, kDepth of them on their way. Bound by
-// memory: 8192 x 28672 with groups of 128 and one right-hand side 22 us, 121 MB at 5.5 TB/s; small ones by what comes
+// memory: 8192 x 28672 with groups of 128 and one right-hand side 22 to 24 us, 121 MB at 5.0 to 5.5 TB/s; small ones by what comes
 // before the first product, 1024 x 8192 5.6 us.
 template <int kDepth, int kParts, bool kZeros, bool kBf16>
 __global__ __launch_bounds__(1024) void endor_q4_gemv_kernel(Q4Params Q) {
@@ -367,7 +369,7 @@ __global__ __launch_bounds__(1024) void endor_q4_gemv_kernel(Q4Params Q) {
 
 // More right-hand sides: x comes from the caches, once for kTiles row tiles. Bound by memory and by the vector ALUs
 // together, which make numbers of codes (9 instructions for 8 codes of fp16, 13 or 21 of bf16) and scale the sums: 28672 x
-// 8192 with 16 right-hand sides, groups of 64 and zeros 25.2 us, 131 MB at 5.2 TB/s; bf16 with groups of 32 42. A second
+// 8192 with 16 right-hand sides, groups of 64 and zeros 25 to 27 us, 131 MB at 4.9 to 5.2 TB/s; bf16 with groups of 32 42. A second
 // block on its way takes as long or longer (8192 x 8192 12.5 us, 13.8 with two), so it is not latency that it waits for.
 template <int kTiles, int kParts, bool kZeros, bool kBf16>
 __global__ __launch_bounds__(512) void endor_q4_gemm_kernel(Q4Params Q) {
