@@ -106,7 +106,8 @@ def _dtype_code(dtype):
 class KVCache:
     """A paged cache: k and v are pools of pages [pages, kv_heads, page_size, head_dim] (any strides whose last is 1 and
     whose others are multiples of 8 elements; the same for both), `pages` the int32 table [batch, max_pages] of every
-    sequence's pages.  The tensors stay the caller's: what they hold may change between calls, the tensors may not."""
+    sequence's pages.  The tensors stay the caller's: what they hold may change between calls, the tensors may not (another table of pages is
+    another KVCache)."""
 
     def __init__(self, k, v, pages):
         torch = _torch()
@@ -132,6 +133,11 @@ class KVCache:
         c.dtype = _dtype_code(k.dtype)
         self.dtype = k.dtype
         self._at = ctypes.addressof(c)
+
+    def __setattr__(self, name, value):
+        if "_at" in self.__dict__ and name in self.__dict__:  # calls go by the addresses that were taken when it was made
+            raise AttributeError("a KVCache stays as it was made: make another one for other tensors")
+        object.__setattr__(self, name, value)
 
     def _scratch(self, nbytes):
         return _torch().empty(nbytes, dtype=_torch().uint8, device=self.k.device) if nbytes else None
@@ -292,7 +298,7 @@ def kv_evict(cache, lengths, seen, weights, positions, budget, recent, max_len=N
 
 @dataclass
 class Q4Matrix:
-    """A 4-bit weight in the form the products read (device memory)."""
+    """A 4-bit weight in the form the products read (device memory).  It stays as it was made: calls go by the address taken then."""
     rows: int
     cols: int
     group: int
@@ -300,8 +306,16 @@ class Q4Matrix:
     packed: object  # torch.uint8, the tensor of q4_pack
 
     def __post_init__(self):
-        self._packed = (self.packed.data_ptr(), self.packed.numel(), self.packed.get_device())
         self._scratch = {}  # bytes by the number of right-hand sides: a plan's figures, asked for once
+        self._packed = (self.packed.data_ptr(), self.packed.numel(), self.packed.get_device())
+
+    def __setattr__(self, name, value):
+        if "_packed" in self.__dict__ and name in self.__dict__:
+            raise AttributeError("a Q4Matrix stays as it was made: make another one for another weight")
+        object.__setattr__(self, name, value)
+
+    def __reduce__(self):  # a copy goes by its own address
+        return Q4Matrix, (self.rows, self.cols, self.group, self.zeros, self.packed)
 
 
 def _q4_groups(cols, group):
